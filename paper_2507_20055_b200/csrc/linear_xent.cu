@@ -20,30 +20,24 @@
 #include "xent_gemm.cuh"
 
 struct cert_xent {
-    int max_rows = 0, D = 0, V = 0, type = 0, parts = 1, device = 0, pairs = 1, sms = 1;
+    int max_rows = 0, type = 0, device = 0, pairs = 1, sms = 1;
     bool with_grad = false;
-    int Dp = 0;
+    cert::XentSizes size = {};
     cert::OpBuffers mem;
     int *status = nullptr;
     int *pos = nullptr, *idx = nullptr, *tgt = nullptr;   // row -> number among the kept ones (-1: ignored); back; class
     int *counts = nullptr;                                // [0] kept rows, [1] rows with a bad target, [2] ticket
     void *xc = nullptr;                                   // [rows_pad][parts * Dp] kept rows
     float2 *partial = nullptr;                            // [slots][rows_pad]
-    size_t partial_cap = 0;
     float *target_logit = nullptr;
     float2 *stat = nullptr;
     double *block_sum = nullptr;
     float *bias32 = nullptr;                              // [V rounded up to 256]
     void *wbuf = nullptr;                                 // [piece][parts * Dp] copy of a piece of the weights
-    size_t wbuf_bytes = 0;
     void *prob = nullptr;                                 // [rows_pad][parts * piece]
-    size_t prob_bytes = 0;
     float *dx32 = nullptr;                                // [splits][rows_pad][Dp]
-    size_t dx32_floats = 0;
     float *dw32 = nullptr;                                // [splits][classes][Dp], where the classes are few
-    size_t dw32_floats = 0;
     float *colsum = nullptr;                              // [rows_pad / 32][piece]
-    size_t colsum_floats = 0;
     // Maps of the workspace for the last call's sizes (encoding one costs the host about as much as a launch's arguments).
     cert::XentMap map_x, map_x_mn, map_p, map_p_mn, map_po, map_dx32, map_dw32;
     int map_rows = -1, map_piece = -1, map_dx_most = 0, map_dw_most = 0;
@@ -55,10 +49,6 @@ struct cert_xent {
 namespace cert {
 namespace {
 
-constexpr size_t kProbBytes = size_t(256) << 20;
-constexpr size_t kWeightBytes = size_t(256) << 20;    // copy of a piece, where every call needs one
-constexpr size_t kWeightBytesSpare = size_t(32) << 20;
-constexpr size_t kSplitBytes = size_t(64) << 20;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kHalfShift = 14;                        // float16 probabilities are stored times 2^14
@@ -446,26 +436,6 @@ xent_finish_kernel(const __grid_constant__ FinishArgs a) {
     }
 }
 
-inline long long up(long long x, long long m) { return (x + m - 1) / m * m; }
-
-// Column tile of the products over a row panel.  For 64 of K a pair's MMAs take 2 bn cycles, and each of its CTAs takes in 128
-// rows of A (fewer where there are fewer) and bn / 2 of B at the 57 bytes per cycle that a multiprocessor gets from L2 (the
-// rate of bulk copies measured with cert_peak_microbench); a tile costs 8 such steps more to start and end.  A width that
-// divides the work into whole waves may win over a wider one (65536 classes, 74 pairs: 293 tiles of 224, four waves, instead
-// of 256 of 256, also four).
-int pick_bn(int rows, int N, int K, int segs, int pairs, int unit) {
-    int best = 256;
-    double cost = 1e30;
-    const int tiles_m = (int)ceil_div_ll(std::max(rows, 1), kXentPairRows);
-    for (int bn = 256; bn >= 64; bn -= unit) {
-        const double waves = (double)ceil_div_ll((long long)tiles_m * ceil_div_ll(N, bn), pairs);
-        const double step = std::max(2.0 * bn, (std::min(rows, 128) * 128.0 + bn * 64.0) / 57.0);
-        const double c = waves * (step * ceil_div_ll(K, 64) * segs + 8 * 512);
-        if (c < cost * 0.999) { cost = c; best = bn; }
-    }
-    return best;
-}
-
 // Calls of up to so many rows run in xent_few.cu, the others on the tensor cores.  There a call's time grows with rows x
 // features (about 10 ns per 1000 elements of x, with gradients), here it is launches and, for 16-bit types, far less per element.
 // Ten classes, with gradients, there against here: bfloat16, 256 x 1024 18 us against 30, 2048 x 1024 31 against 36, 8192 x 256
@@ -492,33 +462,21 @@ void set_segments(XentGemmArgs &g, int parts) {
 
 void pack_weights(cert_xent *op, const void *src, long long ld, int rows, cudaStream_t st) {
     const int vec = aligned(src, 16) && (ld * type_size(op->type)) % 16 == 0;
-    const long long items = (long long)rows * (op->Dp / 8);
+    const XentSizes &size = op->size;
+    const long long items = (long long)rows * (size.Dp / 8);
     const dim3 blocks((unsigned)std::min<long long>(ceil_div_ll(items, 256), (long long)op->sms * 16));
     uint16_t *dst = reinterpret_cast<uint16_t *>(op->wbuf);
     if (op->type == CERT_TYPE_F32)
-        launch_chained(xent_pack_kernel<float>, blocks, dim3(256), 0, st, reinterpret_cast<const float *>(src), ld, rows, op->D, op->Dp, op->parts, dst, vec);
+        launch_chained(xent_pack_kernel<float>, blocks, dim3(256), 0, st, reinterpret_cast<const float *>(src), ld, rows, size.D, size.Dp, size.parts, dst, vec);
     else
-        launch_chained(xent_pack_kernel<uint16_t>, blocks, dim3(256), 0, st, reinterpret_cast<const uint16_t *>(src), ld, rows, op->D, op->Dp, op->parts, dst, vec);
-}
-
-// Column tile and most ranges of K for a gradient's product of tiles_m row panels: as xent_splits, over both.
-void pick_split(int tiles_m, int N, int num_kb, int segs, int pairs, int most, int &bn, int &splits) {
-    double least = 1e30;
-    for (int b = 256; b >= 128; b /= 2) {
-        const int tiles = tiles_m * (int)ceil_div_ll(N, b);
-        const int s = xent_splits(tiles, num_kb, segs, pairs, most);
-        const double waves = (double)ceil_div_ll((long long)tiles * s, pairs);
-        const double cost = waves * ((double)ceil_div_ll(num_kb, s) * segs * (256 + b) / 512 + 8) + (s > 1 ? tiles * s / 8.0 * b / 256 : 0.0);
-        if (cost < least * 0.999) { least = cost; bn = b; splits = s; }
-    }
+        launch_chained(xent_pack_kernel<uint16_t>, blocks, dim3(256), 0, st, reinterpret_cast<const uint16_t *>(src), ld, rows, size.D, size.Dp, size.parts, dst, vec);
 }
 
 cert_status_t run(cert_xent *op, const cert_xent_args_t &q, cudaStream_t st) {
-    const int T = q.rows, D = op->D, V = op->V, Dp = op->Dp, parts = op->parts, es = type_size(op->type);
+    const XentSizes &size = op->size;
+    const int T = q.rows, D = size.D, V = size.V, Dp = size.Dp, parts = size.parts, es = type_size(op->type);
     const bool bf16 = op->type != CERT_TYPE_F16;
     const bool want_grad = q.dx || q.dweight || q.dbias;
-    const int rows_pad = (int)up(std::max(T, 1), kXentPairRows);
-    const int tiles_m = rows_pad / kXentPairRows;
     const int mean = q.reduction == CERT_REDUCE_MEAN;
     const int *count = op->counts;
 
@@ -536,11 +494,9 @@ cert_status_t run(cert_xent *op, const cert_xent_args_t &q, cudaStream_t st) {
         return launch_status();
     }
 
-    // the weights are read in place where TMA can, else piece by piece from a padded copy
     const bool direct = parts == 1 && aligned(q.weight, 16) && (q.ldw * es) % 16 == 0;
-    const long long row_bytes = (long long)parts * Dp * 2;
-    const int Vp = (int)up(V, 256);
-    const int copy_piece = direct ? Vp : (int)std::min<long long>(Vp, (long long)(op->wbuf_bytes / row_bytes) / 256 * 256);
+    const XentPlan plan = xent_plan(size, T, direct, want_grad, op->pairs);
+    const int rows_pad = plan.rows_pad, tiles_m = plan.tiles_m, copy_piece = plan.copy_piece, piece = plan.piece, pieces = plan.pieces;
 
     XentMap map_w = {}, map_w_mn = {};
     XentGemmArgs base = {};
@@ -554,22 +510,9 @@ cert_status_t run(cert_xent *op, const cert_xent_args_t &q, cudaStream_t st) {
     set_segments(base, parts);
 
     // ---- the gradient's pieces and splits
-    const long long prob_row = (long long)rows_pad * parts * 2;
-    const int piece = !want_grad ? Vp : (int)std::min<long long>(copy_piece, std::min<long long>(Vp, (long long)(op->prob_bytes / prob_row) / 256 * 256));
-    const int pieces = (int)ceil_div_ll(V, piece);
     const float unscale = q.grad_scale * (bf16 ? 1.0f : 1.0f / (1 << kHalfShift));
-    const size_t slab = (size_t)rows_pad * Dp, dw_slab = (size_t)std::min(piece, V) * Dp;
-    const int dx_kb = (int)ceil_div_ll(std::min(piece, V), 64);
-    int bn_dx = 256, dx_most = 1, bn_dw = 256, dw_most = 1;
-    if (want_grad) {
-        // where the row and column tiles are too few, K is split and the slabs are added afterwards
-        pick_split(tiles_m, D, dx_kb, base.segs, op->pairs, (int)std::min<size_t>(32, std::max<size_t>(1, op->dx32_floats / slab)), bn_dx, dx_most);
-        const int tiles_v = (int)ceil_div_ll(std::min(piece, V), kXentPairRows);
-        pick_split(tiles_v, D, rows_pad / 64, base.segs, op->pairs,
-                   pieces == 1 ? (int)std::min<size_t>(32, std::max<size_t>(1, op->dw32_floats / dw_slab)) : 1, bn_dw, dw_most);
-        // (fewer rows may count than there are: the device may want more ranges than the host)
-        if (dx_most > 1) dx_most = (int)std::min<size_t>(32, op->dx32_floats / slab);
-    }
+    const size_t slab = plan.slab, dw_slab = plan.dw_slab;
+    const int dx_kb = plan.dx_kb, bn_dx = plan.bn_dx, dx_most = plan.dx_most, bn_dw = plan.bn_dw, dw_most = plan.dw_most;
     const bool dx_direct = pieces == 1 && dx_most == 1, dw_direct = dw_most == 1;
     if (op->map_rows != T || op->map_piece != (want_grad ? piece : 0) || op->map_dx_most != dx_most || op->map_dw_most != dw_most) {
         op->map_rows = -1;
@@ -595,7 +538,7 @@ cert_status_t run(cert_xent *op, const cert_xent_args_t &q, cudaStream_t st) {
         g.ldx = q.ldx; g.D = D; g.Dp = Dp; g.parts = parts;
         g.vec_ok = aligned(q.x, 16) && (q.ldx * es) % 16 == 0;
         g.xc = reinterpret_cast<uint16_t *>(op->xc);
-        g.bias = q.bias; g.bias_type = op->type; g.Vp = Vp; g.bias32 = op->bias32;
+        g.bias = q.bias; g.bias_type = op->type; g.Vp = size.Vp; g.bias32 = op->bias32;
         g.dx_zero = dx_direct ? q.dx : nullptr;
         g.lddx = q.lddx;
         const int by_rows = std::max(1, std::min(op->sms * 4, T));
@@ -604,16 +547,11 @@ cert_status_t run(cert_xent *op, const cert_xent_args_t &q, cudaStream_t st) {
         else launch_chained(xent_begin_kernel<uint16_t>, blocks, dim3(256), 0, st, reinterpret_cast<const uint16_t *>(q.x), g);
     }
 
-    // ROW saves a second product of the logits but its warps wait for one another.  With against without it, bfloat16, 8192
-    // rows, 4096 features, with gradients: 128 classes 136 us against 150, 256 classes 155 against 154 (float32 408 against 475).
-    // The loss alone would gain from 65 classes on (1024 rows, 1024 features: 64 classes 15.5 us against 16.5, 256 classes 20.7
-    // against 16.7), but then it would not be, to the bit, the loss that the call with gradients returns.
-    const bool by_row = V <= 256 && pieces == 1 && copy_piece >= V;
+    const bool by_row = plan.by_row;
 
     // ---- softmax statistics
     if (!by_row) {
-        int bn = pick_bn(T, std::min(V, copy_piece), D, base.segs, op->pairs, 32);
-        while (bn < 256 && 2 * (size_t)ceil_div_ll(Vp, bn) * rows_pad > op->partial_cap) bn += 32;
+        const int bn = plan.bn_lse;
         int slots = 0;
         for (int c0 = 0; c0 < V; c0 += copy_piece) {
             const int width = std::min(copy_piece, V - c0);
@@ -649,7 +587,7 @@ cert_status_t run(cert_xent *op, const cert_xent_args_t &q, cudaStream_t st) {
     // ---- gradient, one piece of the classes after the other
     for (int c0 = 0; c0 < V; c0 += piece) {
         const int width = std::min(piece, V - c0);
-        const int bn_p = by_row ? (V <= 64 ? 64 : V <= 128 ? 128 : 256) : pick_bn(T, width, D, base.segs, op->pairs, 64);
+        const int bn_p = xent_prob_bn(size, plan, T, width, op->pairs);
         if (direct) {
             if (!xent_make_map(&map_w, q.weight, bf16, D, V, q.ldw, 64, bn_p / 2) ||
                 !xent_make_map(&map_w_mn, q.weight, bf16, D, V, q.ldw, 64, 64))
@@ -790,10 +728,10 @@ cert_status_t cert_xent_create(int max_rows, int features, int classes, int type
     if (max_rows > (1 << 24) || features > (1 << 20) || classes > (1 << 28)) return CERT_ERR_UNSUPPORTED;
     cert_xent *op = new (std::nothrow) cert_xent;
     if (!op) return CERT_ERR_OOM;
-    op->max_rows = max_rows; op->D = features; op->V = classes; op->type = type;
+    op->max_rows = max_rows; op->type = type;
     op->with_grad = with_grad != 0;
-    op->parts = type == CERT_TYPE_F32 ? 3 : 1;
-    op->Dp = (int)up(features, 64);
+    op->size = xent_sizes(max_rows, features, classes, type, op->with_grad);
+    const XentSizes &size = op->size;
     int sms = 0;
     cert_status_t fail = CERT_OK;
     if (cudaGetDevice(&op->device) != cudaSuccess ||
@@ -805,41 +743,24 @@ cert_status_t cert_xent_create(int max_rows, int features, int classes, int type
     }
     op->sms = sms;
     op->pairs = std::max(1, sms / 2);
-    const size_t rows_pad = (size_t)up(max_rows, kXentPairRows);
     op->few_rows = few_rows(type, max_rows, features, classes);
     bool ok = op->mem.alloc(&op->status, 1, true) && op->mem.alloc(&op->counts, 4, true);
     if (ok && op->few_rows > 0) {
         const size_t blocks = (size_t)std::max(xent_few_blocks(op->few_rows, sms), xent_few_blocks(std::min(op->few_rows, 8 * sms), sms));
         ok = op->mem.alloc(&op->few_loss, blocks) && op->mem.alloc(&op->few_db, blocks * kFewClasses) &&
-             op->mem.alloc(&op->few_dw, op->with_grad ? blocks * kFewClasses * (size_t)up(features, 4) : 1);
+             op->mem.alloc(&op->few_dw, op->with_grad ? blocks * kFewClasses * (size_t)xent_up(features, 4) : 1);
     }
     if (op->few_rows < max_rows) {
-        const long long Vp = up(classes, 256);
-        const long long row_bytes = (long long)op->parts * op->Dp * 2;
-        const bool copies = op->parts > 1 || features % 8 != 0;
-        // at least one piece of 256 classes fits whatever the sizes
-        const long long w_want = std::min<long long>(Vp * row_bytes, (long long)(copies ? kWeightBytes : kWeightBytesSpare));
-        op->wbuf_bytes = (size_t)std::max<long long>(w_want, std::min<long long>(Vp, 256) * row_bytes);
-        // two slots per column tile: narrow tiles only where few rows share them
-        op->partial_cap = std::max((size_t)(2 * ceil_div_ll(Vp, 256)) * rows_pad, (size_t)(2 * ceil_div_ll(Vp, 64)) * std::min<size_t>(rows_pad, 1024));
-        // a piece of a float32 call may end with a tile of its own
-        op->partial_cap += (size_t)2 * rows_pad * (size_t)(copies ? ceil_div_ll(Vp * row_bytes, (long long)op->wbuf_bytes) : 1);
+        const size_t rows_pad = size.rows_pad;
         ok = ok && op->mem.alloc(&op->pos, rows_pad) && op->mem.alloc(&op->idx, rows_pad) && op->mem.alloc(&op->tgt, rows_pad) &&
-             op->mem.alloc(reinterpret_cast<unsigned char **>(&op->xc), rows_pad * (size_t)row_bytes, true) &&
-             op->mem.alloc(&op->partial, op->partial_cap) && op->mem.alloc(&op->target_logit, rows_pad) &&
+             op->mem.alloc(reinterpret_cast<unsigned char **>(&op->xc), rows_pad * (size_t)size.row_bytes, true) &&
+             op->mem.alloc(&op->partial, size.partial_cap) && op->mem.alloc(&op->target_logit, rows_pad) &&
              op->mem.alloc(&op->stat, rows_pad) && op->mem.alloc(&op->block_sum, rows_pad / 32) &&
-             op->mem.alloc(&op->bias32, (size_t)Vp) &&
-             op->mem.alloc(reinterpret_cast<unsigned char **>(&op->wbuf), op->wbuf_bytes);
-        if (ok && op->with_grad) {
-            const size_t prob_row = rows_pad * op->parts * 2;
-            op->prob_bytes = std::max(std::min((size_t)Vp * prob_row, kProbBytes), (size_t)std::min<long long>(Vp, 256) * prob_row);
-            op->dx32_floats = std::max(rows_pad * op->Dp, std::min(kSplitBytes / 4, 32 * rows_pad * op->Dp));
-            // dW's sums over many rows are only split where the classes alone give few tiles
-            op->dw32_floats = (size_t)Vp * op->Dp <= (1u << 21) ? std::min<size_t>(kSplitBytes / 4, (size_t)32 * Vp * op->Dp) : 64;
-            op->colsum_floats = op->prob_bytes / (op->parts * 2) / 32;
-            ok = op->mem.alloc(reinterpret_cast<unsigned char **>(&op->prob), op->prob_bytes, true) &&
-                 op->mem.alloc(&op->dx32, op->dx32_floats) && op->mem.alloc(&op->dw32, op->dw32_floats) && op->mem.alloc(&op->colsum, op->colsum_floats);
-        }
+             op->mem.alloc(&op->bias32, (size_t)size.Vp) &&
+             op->mem.alloc(reinterpret_cast<unsigned char **>(&op->wbuf), size.wbuf_bytes);
+        if (ok && op->with_grad)
+            ok = op->mem.alloc(reinterpret_cast<unsigned char **>(&op->prob), size.prob_bytes, true) &&
+                 op->mem.alloc(&op->dx32, size.dx32_floats) && op->mem.alloc(&op->dw32, size.dw32_floats) && op->mem.alloc(&op->colsum, size.colsum_floats);
     }
     if (!ok) fail = CERT_ERR_OOM;
     if (fail == CERT_OK && cudaDeviceSynchronize() != cudaSuccess) { cudaGetLastError(); fail = CERT_ERR_CUDA; }
@@ -857,20 +778,20 @@ cert_status_t cert_xent_run(cert_xent_t *op, const cert_xent_args_t *q, void *st
     if (!op || !q || !q->loss || q->rows < 0) return CERT_ERR_INVALID_ARG;
     if (q->rows > op->max_rows) return CERT_ERR_BATCH_TOO_LARGE;
     if (q->reduction != CERT_REDUCE_MEAN && q->reduction != CERT_REDUCE_SUM) return CERT_ERR_INVALID_ARG;
-    if (!q->weight || q->ldw < op->D || (q->rows > 0 && (!q->x || !q->target || q->ldx < op->D))) return CERT_ERR_INVALID_ARG;
+    if (!q->weight || q->ldw < op->size.D || (q->rows > 0 && (!q->x || !q->target || q->ldx < op->size.D))) return CERT_ERR_INVALID_ARG;
     if (!std::isfinite(q->grad_scale)) return CERT_ERR_INVALID_ARG;
     const size_t es = (size_t)type_size(op->type);
     if ((q->x && !aligned(q->x, es)) || !aligned(q->weight, es) || (q->bias && !aligned(q->bias, es)) ||
         (q->dx && !aligned(q->dx, es)) || (q->dweight && !aligned(q->dweight, es)) || (q->dbias && !aligned(q->dbias, es)) ||
         !aligned(q->target, q->target_is_64 ? 8 : 4) || !aligned(q->loss, 4) || !aligned(q->row_losses, 4))
         return CERT_ERR_INVALID_ARG;
-    if ((q->dx && q->lddx < op->D) || (q->dweight && q->lddw < op->D)) return CERT_ERR_INVALID_ARG;
+    if ((q->dx && q->lddx < op->size.D) || (q->dweight && q->lddw < op->size.D)) return CERT_ERR_INVALID_ARG;
     if ((q->dx || q->dweight || q->dbias) && !op->with_grad) return CERT_ERR_UNSUPPORTED;
 #ifdef CERT_BOUNDS
     {
-        const size_t n = (size_t)q->rows, d = (size_t)op->D;
+        const size_t n = (size_t)q->rows, d = (size_t)op->size.D;
         op->mem.permit({{q->loss, 4}, {q->row_losses, n * 4}, {q->dx, n ? ((n - 1) * q->lddx + d) * es : 0},
-                        {q->dweight, ((size_t)(op->V - 1) * q->lddw + d) * es}, {q->dbias, (size_t)op->V * es}}, op->status);
+                        {q->dweight, ((size_t)(op->size.V - 1) * q->lddw + d) * es}, {q->dbias, (size_t)op->size.V * es}}, op->status);
     }
 #endif
     return run(op, *q, static_cast<cudaStream_t>(stream));

@@ -4,14 +4,13 @@
 #include <cstdint>
 
 #include "common.cuh"
+#include "xent_plan.cuh"
 
 namespace cert {
 
 struct XentMap { alignas(64) unsigned char bytes[128]; };   // a CUtensorMap
 
 enum { XENT_EPI_LSE = 0, XENT_EPI_PROB = 1, XENT_EPI_STORE = 2, XENT_EPI_ROW = 3 };
-
-constexpr int kXentPairRows = 256;   // rows of A per CTA pair
 
 // D[m][n] = sum over k of A[m][k] * B[n][k] with 16-bit operands and fp32 accumulators.
 // A float32 operand is held as three bfloat16 parts side by side, x = x0 + x1 + x2 (8 bits of mantissa each); `segs`
@@ -64,25 +63,6 @@ struct XentGemmArgs {
     const int *count;                // non-null: out_scale is divided by max(1, *count) (mean reduction)
     const int *row_map;              // non-null: row m goes to row row_map[m]
 };
-
-// How many ranges K is cut into where there are fewer tiles than CTA pairs: what the pairs' waves cost in steps of 64 of K,
-// with 8 steps for starting and ending a tile and the slabs' later addition (an eighth of a step per tile and slab).  Only
-// counts that fill one, two, three or four waves are looked at.  The kernels work it out from the number of rows that
-// count, which only the device knows; every thread does, so it is a handful of 32-bit operations.
-__host__ __device__ inline int xent_splits(int tiles, int num_kb, int segs, int pairs, int most) {
-    if (tiles <= 0 || most <= 1) return 1;
-    int best = 1;
-    float least = (float)((tiles + pairs - 1) / pairs) * (float)(num_kb * segs + 8);
-    for (int waves = 1; waves <= 4; ++waves) {
-        int s = pairs * waves / tiles;
-        if (s > most) s = most;
-        if (s > num_kb) s = num_kb;
-        if (s <= best) continue;
-        const float cost = (float)((tiles * s + pairs - 1) / pairs) * (float)((num_kb + s - 1) / s * segs + 8) + 0.125f * (float)(tiles * s);
-        if (cost < least) { least = cost; best = s; }
-    }
-    return best;
-}
 
 bool xent_gemm_prepare();
 bool xent_make_map(XentMap *m, const void *base, bool bf16, long long inner, long long outer, long long pitch_elems,

@@ -1,0 +1,54 @@
+"""Calls of the operators at which workspaces, pieces or types are at their limits; bounds as in test_gpu_operators.py."""
+import os
+import subprocess
+import sys
+
+import pytest
+
+from test_gpu_operators import _xent_case, _xent_check
+
+pytestmark = pytest.mark.gpu
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+@pytest.fixture(scope="module")
+def B():
+    from paper_2507_20055_b200 import binding
+    return binding
+
+
+def _unaligned(t):
+    """The same matrix in memory that starts one element behind a 16-byte boundary."""
+    import torch
+    flat = torch.empty(t.numel() + 1, dtype=t.dtype, device=t.device)
+    view = flat[1:].view(t.shape)
+    view.copy_(t)
+    return view
+
+
+@pytest.mark.parametrize("kind,rows,features,classes", [("bfloat16", 3500, 4096, 32768), ("float16", 3329, 2048, 32768), ("bfloat16", 300, 4096, 12000)])
+def test_xent_copied_weights_in_pieces_of_narrow_tiles(B, kind, rows, features, classes):
+    """Weights that TMA cannot read in place go through a copy of a few thousand classes, whose tiles leave more pairs than
+    one tiling of all classes."""
+    x, w, y, b = _xent_case(kind, rows, features, classes, True, 0.0, seed=17)
+    op = B.LinearCrossEntropy(rows, features, classes, dtype=x.dtype)
+    w = _unaligned(w)
+    assert w.data_ptr() % 16 == 2
+    _xent_check(B, op, x, w, y, b)
+    # rows that do not count leave the number of slots as it is
+    y[::3] = -100
+    _xent_check(B, op, x, w, y, b)
+
+
+def test_xent_in_several_pieces_under_the_checking_build():
+    """Every plain store of the piecewise calls is looked up in the table of the buffers that they may write."""
+    if os.environ.get("CERT_EXPECT_CHECKED") == "1":
+        pytest.skip("already a run of the checking build")
+    from paper_2507_20055_b200 import build
+    env = dict(os.environ, CERT_LIB=build.build_checked(), CERT_EXPECT_CHECKED="1")
+    run = subprocess.run([sys.executable, "-m", "pytest", os.path.join("tests", "test_gpu_operators.py"), os.path.join("tests", "test_gpu_operators_edges.py"),
+                          "-q", "-x", "-m", "gpu", "-k", "xent_in_several_pieces or xent_copied_weights"], cwd=ROOT, env=env, capture_output=True,
+                         text=True, timeout=900)
+    assert run.returncode == 0, run.stdout[-3000:] + run.stderr[-2000:]
+    assert " passed" in run.stdout
