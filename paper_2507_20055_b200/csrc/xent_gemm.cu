@@ -469,7 +469,7 @@ xent_gemm_kernel(const __grid_constant__ CUtensorMap map_a0, const __grid_consta
                     tmem_ld_wait();
                 }
                 if (EPI == XENT_EPI_LSE || EPI == XENT_EPI_PROB) {
-                    if (a.bias) {
+                    if (a.bias && xent_reads_bias(col0, a.N)) {
 #pragma unroll
                         for (int g = 0; g < 8; ++g) {
                             const float4 b4 = __ldg(reinterpret_cast<const float4 *>(a.bias + col0) + g);

@@ -30,7 +30,7 @@ struct XentGemmArgs {
     int bf16;                        // operand type: bfloat16, else float16
     int *status;
     // LSE and PROB: the logits are acc + bias[n]; column n of this launch is class class0 + n
-    const float *bias;               // fp32, readable up to the end of the last column tile; or null
+    const float *bias;               // fp32, readable up to N rounded up to 32 (ROW: to the tile's end); or null
     int class0;
     const int *target;               // [rows] class of each row
     // LSE: per row and slot (two slots per column tile) the running maximum (log2 units) and sum; target's logit

@@ -162,6 +162,10 @@ inline XentPlan xent_plan(const XentSizes &s, int rows, bool direct, bool want_g
     return p;
 }
 
+// Whether the 32 columns from col0 on of a piece of N classes read the bias: the float32 copy of it ends at V rounded up to
+// 256, the last piece's last tile may end behind that (its columns from N on are no classes).
+CERT_BOTH inline bool xent_reads_bias(int col0, int N) { return col0 < N; }
+
 // Column tile of a piece's probabilities.
 inline int xent_prob_bn(const XentSizes &s, const XentPlan &p, int rows, int width, int pairs) {
     return p.by_row ? (s.V <= 64 ? 64 : s.V <= 128 ? 128 : 256) : xent_pick_bn(rows, width, s.D, p.segs, pairs, 64);

@@ -41,6 +41,12 @@ def test_xent_copied_weights_in_pieces_of_narrow_tiles(B, kind, rows, features, 
     _xent_check(B, op, x, w, y, b)
 
 
+@pytest.mark.parametrize("rows,features,classes,aligned", [(3072, 64, 44544, True), (546, 3600, 12750, False)])
+def test_xent_last_piece_with_a_tile_behind_the_bias(B, rows, features, classes, aligned):
+    x, w, y, b = _xent_case("bfloat16", rows, features, classes, True, 0.2, seed=23)
+    _xent_check(B, B.LinearCrossEntropy(rows, features, classes, dtype=x.dtype), x, w if aligned else _unaligned(w), y, b)
+
+
 def test_xent_in_several_pieces_under_the_checking_build():
     """Every plain store of the piecewise calls is looked up in the table of the buffers that they may write."""
     if os.environ.get("CERT_EXPECT_CHECKED") == "1":
@@ -48,7 +54,7 @@ def test_xent_in_several_pieces_under_the_checking_build():
     from paper_2507_20055_b200 import build
     env = dict(os.environ, CERT_LIB=build.build_checked(), CERT_EXPECT_CHECKED="1")
     run = subprocess.run([sys.executable, "-m", "pytest", os.path.join("tests", "test_gpu_operators.py"), os.path.join("tests", "test_gpu_operators_edges.py"),
-                          "-q", "-x", "-m", "gpu", "-k", "xent_in_several_pieces or xent_copied_weights"], cwd=ROOT, env=env, capture_output=True,
+                          "-q", "-x", "-m", "gpu", "-k", "xent_in_several_pieces or xent_copied_weights or xent_last_piece"], cwd=ROOT, env=env, capture_output=True,
                          text=True, timeout=900)
     assert run.returncode == 0, run.stdout[-3000:] + run.stderr[-2000:]
     assert " passed" in run.stdout

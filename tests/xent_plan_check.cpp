@@ -25,6 +25,8 @@ extern "C" int check_call(int max_rows, int rows, int d, int v, int type, int di
         for (int c0 = 0; c0 < v; c0 += p.copy_piece) {
             const int width = std::min(p.copy_piece, v - c0);
             slots += 2 * xent_div(width, p.bn_lse);
+            for (int col0 = 0; col0 < width; col0 += 32)
+                if (xent_reads_bias(col0, width)) FITS("bias read for statistics", c0 + col0 + 32, s.Vp);
         }
         FITS("slots", slots * p.rows_pad, s.partial_cap);
         FITS("slots counted", xent_slots(v, p.copy_piece, p.bn_lse), slots);
@@ -37,6 +39,12 @@ extern "C" int check_call(int max_rows, int rows, int d, int v, int type, int di
         FITS("column sums", (long long)p.rows_pad / 32 * p.piece, s.colsum_floats);
         FITS("dx sums", (long long)p.dx_most * (long long)p.slab, s.dx32_floats);
         if (p.dw_most > 1) FITS("dW sums", (long long)p.dw_most * (long long)p.dw_slab, s.dw32_floats);
+        for (int c0 = 0; c0 < v; c0 += p.piece) {
+            const int width = std::min(p.piece, v - c0), bn = xent_prob_bn(s, p, rows, width, pairs);
+            const int end = (int)std::min<long long>(xent_up(width, bn), p.by_row ? bn : p.piece);
+            for (int col0 = 0; col0 < end; col0 += 32)
+                if (p.by_row || xent_reads_bias(col0, width)) FITS("bias read for probabilities", c0 + col0 + 32, s.Vp);
+        }
         FITS("pieces", p.piece, p.copy_piece);
         FITS("piece in tiles of 256", p.piece % 256, 0);
     }
