@@ -497,8 +497,8 @@ cert_status_t cert_clip_destroy(cert_clip_t *op);
  * once for every 16 rows (8 in float32).
  *   cert_int4_create   codes [out_features][(in_features + 1) / 2] bytes (even k in the low four bits), scales
  *            [out_features][ceil(in_features / group)] of `type`, zeros [same] bytes or NULL (8 everywhere); group 32, 64, 128
- *            or 256; all contiguous.  They are laid out again for the kernels once, on `stream`; the originals may be freed
- *            when the stream has come past it.
+ *            or 256; all contiguous.  They are laid out again for the kernels once, on `stream`, and the call waits until that
+ *            is done: the originals may be freed at once, and any stream may run the product.
  *   cert_int4_matvec   x [rows][in_features] with rows ldx apart, y [rows][out_features] with rows ldy apart, bias
  *            [out_features] or NULL, all of `type`.  The products take x as float16 times a power of two per row (bfloat16:
  *            off by at most 2^-40 of the row's largest value; float32: two float16 parts, 22 bits), sums are fp32, the

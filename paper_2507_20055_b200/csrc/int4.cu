@@ -740,16 +740,19 @@ cert_status_t cert_int4_create(const unsigned char *codes, const void *scales, c
 #ifdef CERT_BOUNDS
     op->mem.permit({}, op->status);
 #endif
-    // plain launches: these kernels have ended before any later one on the stream begins (the product reads the weights
-    // before it waits for the kernel in front of it)
     int4_repack_kernel<<<blocks_for(words, op->sms), 256, 0, st>>>(codes, shape, op->records, words);
     if (type == CERT_TYPE_F32)
         int4_repack_groups_kernel<<<blocks_for(gs, op->sms), 256, 0, st>>>(reinterpret_cast<const float *>(scales), zeros, shape, op->records, gs);
     else
         int4_repack_groups_kernel<<<blocks_for(gs, op->sms), 256, 0, st>>>(reinterpret_cast<const uint16_t *>(scales), zeros, shape, op->records, gs);
-    const cert_status_t s = launch_status();
+    cert_status_t s = launch_status();
+    // The product's copying warp reads the records before it waits for the kernel in front of it, and only what the host has
+    // seen to be complete is sure to be visible to it then.
+    if (cudaDeviceSynchronize() != cudaSuccess) {
+        cudaGetLastError();
+        if (s == CERT_OK) s = CERT_ERR_CUDA;
+    }
     if (s != CERT_OK) {
-        cudaDeviceSynchronize();
         op->mem.release();
         delete op;
         return s;

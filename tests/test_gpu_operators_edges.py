@@ -58,3 +58,22 @@ def test_xent_in_several_pieces_under_the_checking_build():
                          text=True, timeout=900)
     assert run.returncode == 0, run.stdout[-3000:] + run.stderr[-2000:]
     assert " passed" in run.stdout
+
+
+def test_int4_weights_are_laid_out_when_the_constructor_returns(B):
+    """The product reads them ahead of the wait for the kernel in front of it, on whatever stream: nothing may be under way."""
+    import torch
+    codes = torch.randint(0, 256, (4096, 2048), device="cuda", dtype=torch.uint8)
+    scales = torch.full((4096, 64), 0.01, dtype=torch.bfloat16, device="cuda")
+    big = torch.randn(8192, 8192, device="cuda")
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        for _ in range(20):
+            big @ big                                      # some 300 ms in front of the layout
+        op = B.Int4Weight(codes, scales, 4096, 64)
+        assert side.query()
+    x = torch.randn(1, 4096, device="cuda").to(torch.bfloat16)
+    first = op.matvec(x)
+    torch.cuda.synchronize()
+    assert bool((op.matvec(x) == first).all()) and op.last_status() == 0
