@@ -48,6 +48,7 @@ struct __align__(16) Bars {
     uint64_t empty[kMaxStages];
     uint64_t acc_full[2];
     uint64_t acc_empty[2];
+    uint64_t row_meet[4];                // ROW: the two warps of a quarter
     uint32_t tmem_base;
     uint32_t abort_flag;
 };
@@ -118,6 +119,16 @@ __device__ __forceinline__ bool pipe_wait(uint32_t bar, uint32_t parity, volatil
         if (__any_sync(0xffffffffu, out)) return false;
         if (ready) return true;
     }
+}
+
+// Two warps meet: both have written, or read, what they share before either goes on.  A warp that gave up elsewhere never comes,
+// so this wait has its limit too (a hardware barrier has none).
+__device__ __forceinline__ bool pair_meet(uint64_t *bar, uint32_t &phase, int lane, volatile uint32_t *abort_flag) {
+    __syncwarp();
+    if (lane == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory");
+    const bool met = pipe_wait(smem_u32(bar), phase, abort_flag);
+    phase ^= 1;
+    return met;
 }
 
 // One lane of a converged warp.  The producer and the MMA issuer run as whole warps and elect a lane for the instruction
@@ -193,6 +204,8 @@ xent_gemm_kernel(const __grid_constant__ CUtensorMap map_a0, const __grid_consta
             mbar_init(&bars->acc_full[i], 1);
             mbar_init(&bars->acc_empty[i], kEpiWarps * 2);
         }
+        if (EPI == XENT_EPI_ROW)
+            for (int i = 0; i < 4; ++i) mbar_init(&bars->row_meet[i], 2);
         bars->abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -340,6 +353,7 @@ xent_gemm_kernel(const __grid_constant__ CUtensorMap map_a0, const __grid_consta
         const uint32_t acc_empty0 = map_to_cta(smem_u32(&bars->acc_empty[0]), 0);
         uint8_t *slab = slabs + (warp - 2) * slab_bytes;
         int turn = 0;                                          // which half of the slab the next 16-bit block takes
+        uint32_t met = 0;                                      // phase of the meetings with the quarter's other warp
         bool ok = true;
         int lt = 0;
         for (int t = group; t < total && ok; t += n_groups) {
@@ -427,9 +441,9 @@ xent_gemm_kernel(const __grid_constant__ CUtensorMap map_a0, const __grid_consta
                 }
                 float4 *half_row = reinterpret_cast<float4 *>(bars + 1) + quarter * 32 + lane;    // [half][row]: maximum, sum, target
                 half_row[half * BM] = make_float4(m_half, s_half, zt, 0.0f);
-                asm volatile("bar.sync %0, 64;" ::"r"(1 + quarter) : "memory");
+                if (!pair_meet(&bars->row_meet[quarter], met, lane, abort_flag)) { ok = false; break; }
                 const float4 h0 = half_row[0], h1 = half_row[BM];
-                asm volatile("bar.sync %0, 64;" ::"r"(1 + quarter) : "memory");      // read before the next tile's
+                if (!pair_meet(&bars->row_meet[quarter], met, lane, abort_flag)) { ok = false; break; }      // read before the next tile's
                 const float m = fmaxf(h0.x, h1.x), sub = m == -INFINITY ? 0.0f : m;
                 const float s = h0.y * ex2(h0.x - sub) + h1.y * ex2(h1.x - sub), l2s = log2f(s);
                 double nll = 0.0;
