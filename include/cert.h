@@ -396,8 +396,9 @@ cert_status_t cert_peak_microbench(int kind, double target_ms, double *tflops_ou
  * Operators next to the certifiers (no counterpart in the paper): what a user needs to train the networks
  * whose bounds the calls above compute, and to run them as they are stored.  All pointers are DEVICE pointers
  * unless marked HOST; work is enqueued on `stream` (a cudaStream_t, NULL = the default stream), the calls do not
- * wait and, after create, allocate nothing.  A handle belongs to the device that is current at its creation; two
- * calls on one handle must not overlap on the device (they share its workspace).
+ * wait and, after create, allocate nothing.  A handle belongs to the device that is current at its creation, and a
+ * call with another device current is refused (CERT_ERR_INVALID_ARG); two calls on one handle must not overlap on the device
+ * (they share its workspace).
  * ====================================================================================================== */
 
 /* Element types of the operators' matrices. */

@@ -466,9 +466,27 @@ def _empty(shape, dtype, device, stream, like=None):
     return torch.empty(*shape, dtype=dtype, device=device) if shape else torch.empty(shape, dtype=dtype, device=device)
 
 
+def _call(device, function, *args):
+    """The library's answer with `device` current: a handle belongs to one device, whose default stream is 0 like every other's."""
+    global _current_device
+    if _current_device is None:
+        import torch
+        _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+    if _current_device() == device.index:
+        return function(*args)
+    import torch
+    with torch.cuda.device(device):
+        return function(*args)
+
+
+_current_device = None
+
+
 def _stream_ptr(stream, device):
     """The stream's handle.  (The current stream's is looked up without making a Stream object, a third of a small call.)"""
     if stream is not None:
+        if stream.device != device:
+            raise ValueError(f"stream: of {stream.device}, the operator is on {device}")
         return stream.cuda_stream
     global _current_raw_stream
     if _current_raw_stream is None:
@@ -525,7 +543,7 @@ class LinearCrossEntropy:
         out = _empty((x.shape[0] + 1,), torch.float32, self.device, stream)
         q.loss = out.data_ptr()
         q.row_losses = q.loss + 4
-        _check(_lib.cert_xent_run(self._h, ctypes.byref(q), _stream_ptr(stream, self.device)), "cert_xent_run")
+        _check(_call(self.device, _lib.cert_xent_run, self._h, ctypes.byref(q), _stream_ptr(stream, self.device)), "cert_xent_run")
         return out[0], out[1:]
 
     def loss_and_grad(self, x, weight, target, bias=None, ignore_index: int = -100, reduction: str = "mean",
@@ -556,19 +574,19 @@ class LinearCrossEntropy:
         if row_losses is not None:
             _check_rows("row_losses", row_losses, (x.shape[0],), torch.float32, device)
             q.row_losses = row_losses.data_ptr()
-        _check(_lib.cert_xent_run(self._h, ctypes.byref(q), _stream_ptr(stream, device)), "cert_xent_run")
+        _check(_call(self.device, _lib.cert_xent_run, self._h, ctypes.byref(q), _stream_ptr(stream, device)), "cert_xent_run")
         return loss, dx, dweight, dbias
 
     def last_status(self, stream=None) -> int:
         """0, or what went wrong in an earlier call on this object (1: a target outside the classes); clears it."""
-        return int(_lib.cert_xent_last_status(self._h, _stream_ptr(stream, self.device)))
+        return int(_call(self.device, _lib.cert_xent_last_status, self._h, _stream_ptr(stream, self.device)))
 
     def check_guards(self, stream=None) -> int:
-        return int(_lib.cert_xent_check_guards(self._h, _stream_ptr(stream, self.device)))
+        return int(_call(self.device, _lib.cert_xent_check_guards, self._h, _stream_ptr(stream, self.device)))
 
     def destroy(self):
         if getattr(self, "_h", None):
-            _check(_lib.cert_xent_destroy(self._h), "cert_xent_destroy")
+            _check(_call(self.device, _lib.cert_xent_destroy, self._h), "cert_xent_destroy")
             self._h = None
 
     def __del__(self):
@@ -615,18 +633,18 @@ class GradClipper:
             norm_out = _empty((), torch.float32, self.device, stream, self._number)
         elif norm_out.device != self.device or norm_out.dtype != torch.float32 or norm_out.numel() != 1:
             raise ValueError("norm_out: one float32 number on the tensors' device is required")
-        _check(_lib.cert_clip_run(self._h, float(max_norm), norm_out.data_ptr(), _stream_ptr(stream, self.device)), "cert_clip_run")
+        _check(_call(self.device, _lib.cert_clip_run, self._h, float(max_norm), norm_out.data_ptr(), _stream_ptr(stream, self.device)), "cert_clip_run")
         return norm_out
 
     def last_status(self, stream=None) -> int:
-        return int(_lib.cert_clip_last_status(self._h, _stream_ptr(stream, self.device)))
+        return int(_call(self.device, _lib.cert_clip_last_status, self._h, _stream_ptr(stream, self.device)))
 
     def check_guards(self, stream=None) -> int:
-        return int(_lib.cert_clip_check_guards(self._h, _stream_ptr(stream, self.device)))
+        return int(_call(self.device, _lib.cert_clip_check_guards, self._h, _stream_ptr(stream, self.device)))
 
     def destroy(self):
         if getattr(self, "_h", None):
-            _check(_lib.cert_clip_destroy(self._h), "cert_clip_destroy")
+            _check(_call(self.device, _lib.cert_clip_destroy, self._h), "cert_clip_destroy")
             self._h = None
 
     def __del__(self):
@@ -700,7 +718,7 @@ class Int4Weight:
             out = _empty((rows, self.out_features), self.dtype, self.device, stream)
         else:
             _check_rows("out", out, (rows, self.out_features), self.dtype, self.device)
-        _check(_lib.cert_int4_matvec(self._h, x.data_ptr(), _ld(x), rows, bias.data_ptr() if bias is not None else None,
+        _check(_call(self.device, _lib.cert_int4_matvec, self._h, x.data_ptr(), _ld(x), rows, bias.data_ptr() if bias is not None else None,
                                      int(bool(relu)), out.data_ptr(), _ld(out), _stream_ptr(stream, self.device)),
                "cert_int4_matvec")
         return out
@@ -709,18 +727,18 @@ class Int4Weight:
         """The weights as float32: what a CertNet of the stored network is made from."""
         import torch
         w = _empty((self.out_features, self.in_features), torch.float32, self.device, stream)
-        _check(_lib.cert_int4_dequantize(self._h, w.data_ptr(), _stream_ptr(stream, self.device)), "cert_int4_dequantize")
+        _check(_call(self.device, _lib.cert_int4_dequantize, self._h, w.data_ptr(), _stream_ptr(stream, self.device)), "cert_int4_dequantize")
         return w
 
     def last_status(self, stream=None) -> int:
-        return int(_lib.cert_int4_last_status(self._h, _stream_ptr(stream, self.device)))
+        return int(_call(self.device, _lib.cert_int4_last_status, self._h, _stream_ptr(stream, self.device)))
 
     def check_guards(self, stream=None) -> int:
-        return int(_lib.cert_int4_check_guards(self._h, _stream_ptr(stream, self.device)))
+        return int(_call(self.device, _lib.cert_int4_check_guards, self._h, _stream_ptr(stream, self.device)))
 
     def destroy(self):
         if getattr(self, "_h", None):
-            _check(_lib.cert_int4_destroy(self._h), "cert_int4_destroy")
+            _check(_call(self.device, _lib.cert_int4_destroy, self._h), "cert_int4_destroy")
             self._h = None
 
     def __del__(self):

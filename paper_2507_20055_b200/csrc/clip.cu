@@ -300,7 +300,7 @@ cert_status_t cert_clip_create(const cert_tensor_t *tensors, int n, void *const 
 
 cert_status_t cert_clip_run(cert_clip_t *op, float max_norm, float *norm_out, void *stream) {
     using namespace cert;
-    if (!op || !norm_out || !aligned(norm_out, 4) || !(max_norm >= 0.0f)) return CERT_ERR_INVALID_ARG;
+    if (!op || !norm_out || !aligned(norm_out, 4) || !(max_norm >= 0.0f) || !on_device(op->device)) return CERT_ERR_INVALID_ARG;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
 #ifdef CERT_BOUNDS
     {
@@ -323,16 +323,16 @@ cert_status_t cert_clip_run(cert_clip_t *op, float max_norm, float *norm_out, vo
 }
 
 cert_status_t cert_clip_last_status(cert_clip_t *op, void *stream) {
-    if (!op) return CERT_ERR_INVALID_ARG;
+    if (!op || !cert::on_device(op->device)) return CERT_ERR_INVALID_ARG;
     return cert::read_status(op->status, static_cast<cudaStream_t>(stream));
 }
 
 int cert_clip_check_guards(cert_clip_t *op, void *stream) {
-    return op ? op->mem.check(static_cast<cudaStream_t>(stream)) : -1;
+    return op && cert::on_device(op->device) ? op->mem.check(static_cast<cudaStream_t>(stream)) : -1;
 }
 
 cert_status_t cert_clip_destroy(cert_clip_t *op) {
-    if (!op) return CERT_ERR_INVALID_ARG;
+    if (!op || !cert::on_device(op->device)) return CERT_ERR_INVALID_ARG;
     const bool ok = cudaDeviceSynchronize() == cudaSuccess;
     if (!ok) cudaGetLastError();
     const bool freed = op->mem.release();

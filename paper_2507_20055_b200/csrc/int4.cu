@@ -764,7 +764,7 @@ cert_status_t cert_int4_create(const unsigned char *codes, const void *scales, c
 cert_status_t cert_int4_matvec(cert_int4_t *op, const void *x, long long ldx, int rows, const void *bias, int relu, void *y,
                                long long ldy, void *stream) {
     using namespace cert;
-    if (!op || rows < 0) return CERT_ERR_INVALID_ARG;
+    if (!op || rows < 0 || !on_device(op->device)) return CERT_ERR_INVALID_ARG;
     if (rows == 0) return CERT_OK;
     const size_t es = (size_t)type_size(op->type);
     if (!x || !y || ldx < op->K || ldy < op->N || !aligned(x, es) || !aligned(y, es) || !aligned(bias, es)) return CERT_ERR_INVALID_ARG;
@@ -790,7 +790,7 @@ cert_status_t cert_int4_matvec(cert_int4_t *op, const void *x, long long ldx, in
 
 cert_status_t cert_int4_dequantize(cert_int4_t *op, float *weight, void *stream) {
     using namespace cert;
-    if (!op || !weight || !aligned(weight, 4)) return CERT_ERR_INVALID_ARG;
+    if (!op || !weight || !aligned(weight, 4) || !on_device(op->device)) return CERT_ERR_INVALID_ARG;
 #ifdef CERT_BOUNDS
     op->mem.permit({{weight, (size_t)op->N * op->K * 4}}, op->status);
 #endif
@@ -827,16 +827,16 @@ cert_status_t cert_int4_quantize(const void *weight, long long ldw, int out_feat
 }
 
 cert_status_t cert_int4_last_status(cert_int4_t *op, void *stream) {
-    if (!op) return CERT_ERR_INVALID_ARG;
+    if (!op || !cert::on_device(op->device)) return CERT_ERR_INVALID_ARG;
     return cert::read_status(op->status, static_cast<cudaStream_t>(stream));
 }
 
 int cert_int4_check_guards(cert_int4_t *op, void *stream) {
-    return op ? op->mem.check(static_cast<cudaStream_t>(stream)) : -1;
+    return op && cert::on_device(op->device) ? op->mem.check(static_cast<cudaStream_t>(stream)) : -1;
 }
 
 cert_status_t cert_int4_destroy(cert_int4_t *op) {
-    if (!op) return CERT_ERR_INVALID_ARG;
+    if (!op || !cert::on_device(op->device)) return CERT_ERR_INVALID_ARG;
     const bool ok = cudaDeviceSynchronize() == cudaSuccess;
     if (!ok) cudaGetLastError();
     const bool freed = op->mem.release();

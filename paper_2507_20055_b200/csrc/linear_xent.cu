@@ -775,7 +775,7 @@ cert_status_t cert_xent_create(int max_rows, int features, int classes, int type
 
 cert_status_t cert_xent_run(cert_xent_t *op, const cert_xent_args_t *q, void *stream) {
     using namespace cert;
-    if (!op || !q || !q->loss || q->rows < 0) return CERT_ERR_INVALID_ARG;
+    if (!op || !q || !q->loss || q->rows < 0 || !on_device(op->device)) return CERT_ERR_INVALID_ARG;
     if (q->rows > op->max_rows) return CERT_ERR_BATCH_TOO_LARGE;
     if (q->reduction != CERT_REDUCE_MEAN && q->reduction != CERT_REDUCE_SUM) return CERT_ERR_INVALID_ARG;
     if (!q->weight || q->ldw < op->size.D || (q->rows > 0 && (!q->x || !q->target || q->ldx < op->size.D))) return CERT_ERR_INVALID_ARG;
@@ -798,16 +798,16 @@ cert_status_t cert_xent_run(cert_xent_t *op, const cert_xent_args_t *q, void *st
 }
 
 cert_status_t cert_xent_last_status(cert_xent_t *op, void *stream) {
-    if (!op) return CERT_ERR_INVALID_ARG;
+    if (!op || !cert::on_device(op->device)) return CERT_ERR_INVALID_ARG;
     return cert::read_status(op->status, static_cast<cudaStream_t>(stream));
 }
 
 int cert_xent_check_guards(cert_xent_t *op, void *stream) {
-    return op ? op->mem.check(static_cast<cudaStream_t>(stream)) : -1;
+    return op && cert::on_device(op->device) ? op->mem.check(static_cast<cudaStream_t>(stream)) : -1;
 }
 
 cert_status_t cert_xent_destroy(cert_xent_t *op) {
-    if (!op) return CERT_ERR_INVALID_ARG;
+    if (!op || !cert::on_device(op->device)) return CERT_ERR_INVALID_ARG;
     const bool ok = cudaDeviceSynchronize() == cudaSuccess;
     if (!ok) cudaGetLastError();
     const bool freed = op->mem.release();

@@ -94,6 +94,17 @@ private:
 #endif
 };
 
+// Whether the device that a handle was made on is current: with another one, the default stream is that device's, and a launch
+// would get pointers of this one.
+inline bool on_device(int device) {
+    int current = -1;
+    if (cudaGetDevice(&current) != cudaSuccess) {
+        cudaGetLastError();
+        return false;
+    }
+    return current == device;
+}
+
 // The status word of a handle as a return code; clears it.
 inline cert_status_t read_status(int *status_dev, cudaStream_t st) {
     int s = 0;
