@@ -6,13 +6,14 @@
 // K of it) in shared memory and streams its rows' records, 8 to a stage, one for each of half its 16 warps; a 17th warp
 // copies whole stages with cp.async.bulk as far ahead as shared memory goes, and three more add up the warps' sums, so that
 // the 16 never wait for one another.  The products run on mma.sync in float16, weights as the 16-row operand, x as its
-// 8 columns.  A code becomes a float16 with one AND-OR: 1024 + code, or 1024 + 16 code four bits higher (bfloat16's mantissa
-// has no room for the second form).  x goes in as float16 times a power of two per row, which puts the row's largest value
-// below 2^15: a bfloat16's eight bits stay exact down to 2^-29 of the largest and are off by at most 2^-40 of it below;
-// a float32 takes two columns, hi and lo, 22 bits.  A group's sum is multiplied by its scale in fp32; the warps' sums are
-// added in a fixed order.
-// Measured: 28672 x 8192 in groups of 128, bfloat16, one row of x: 26.7 us, 121 MB of records at 4.5 TB/s; the copies alone, without
-// the products, 21 us.  11009 x 4096 in groups of 64 with zero points, float16, 13 rows: 15.4 us (floor of the bytes 3.8), the
+// 8 columns.  A code becomes a float16 with one AND-OR, 1024 + code, or 1024 + 16 code four bits higher (bfloat16's mantissa
+// has no room for the second form), and one multiply-add that takes the constant and the zero point off; 1024 plus an integer in
+// the last bits is the published way to do this (Kim, Henry, Fahim and Awadalla 2022, Who Says Elephants Can't Run).
+// x goes in as float16 times a power of two per row, which puts the row's largest value below 2^15: a bfloat16's eight bits stay
+// exact down to 2^-29 of the largest and are off by at most 2^-40 of it below; a float32 takes two columns, hi and lo, 22 bits.
+// A group's sum is multiplied by its scale in fp32; the warps' sums are added in a fixed order.
+// Measured: 28672 x 8192 in groups of 128, bfloat16, one row of x: 29.1 us, 121 MB of records at 4.2 TB/s; the copies alone, without
+// the products, 21 us.  11009 x 4096 in groups of 64 with zero points, float16, 13 rows: 14.8 us (floor of the bytes 3.8), the
 // reads of x from shared memory, 16 columns for each record, and the five rounds of items being what is left.
 #include <algorithm>
 #include <cmath>
@@ -225,7 +226,7 @@ struct Int4Args {
     int panel_chunks, panels;                        // chunks of K whose x is in shared memory at a time
     int x_pitch;                                     // bytes from one column of x to the next
     int stages;
-    int red_off, x_off, xsum_off, out_off;           // in shared memory
+    int red_off, x_off, out_off;                     // in shared memory
     int *status;
 };
 
@@ -288,9 +289,11 @@ __device__ __forceinline__ bool counts_reach(const uint32_t *counts, int least, 
 __device__ __forceinline__ void consumers_meet() { asm volatile("bar.sync 1, %0;" ::"n"(kWarps * 32) : "memory"); }
 
 // NT: column tiles (8 columns each) of the x operand; SHIFT: log2 of the group.
-// For 16-bit x the codes go into the product with their constant, which is taken off a group's sum afterwards, (1024 + zero)
-// times the sum of x; that saves an operation per pair of weights.  It costs seven of the 24 bits of the sums, far below the
-// result's rounding.  A float32 result has no such room: there the codes are made exact first.
+// The codes are made exact, code - zero, before the product.  Left in it with their constant, which a group's sum of x can take
+// off afterwards, they fill the accumulator with up to 1024 times x, and for x of one sign (behind a ReLU) its truncation errors
+// add up: float16, K = 4096, outputs off by 2.5e-4 (groups of 64) to 8.0e-4 (256) of their root mean square, where rounding them
+// alone is 2.1e-4, and so it is now.  28672 x 8192, one row: 29.1 us against 27.8; 11009 x 4096, 13 rows, which needs no
+// sums of x any more: 14.8 against 16.1.
 template <typename T, int NT, bool ZEROS, int SHIFT>
 __global__ void __launch_bounds__(kThreads, 1)
 int4_matvec_kernel(const __grid_constant__ Int4Args a) {
@@ -373,7 +376,6 @@ int4_matvec_kernel(const __grid_constant__ Int4Args a) {
     }
 
     float *red = reinterpret_cast<float *>(smem + a.red_off);         // [kBufs][kWarps][kRed]
-    float *xsum = reinterpret_cast<float *>(smem + a.xsum_off);       // [groups of the panel][COLS]
     pdl_wait();
 
     if (warp > kWarps) {
@@ -470,26 +472,6 @@ int4_matvec_kernel(const __grid_constant__ Int4Args a) {
             }
         }
         consumers_meet();
-        if constexpr (!kF32) {
-            // sums of x over the groups, four lanes per sum, neighbouring 16 bytes
-            for (int i = threadIdx.x >> 2; i < nc * GC * COLS; i += kWarps * 8) {
-                const int g = i / COLS, c = min(i - g * COLS, cols - 1), l = lane & 3;
-                const uint4 *p = reinterpret_cast<const uint4 *>(smem + a.x_off + c * a.x_pitch + (g << SHIFT) * 2);
-                float v = 0.0f;
-#pragma unroll
-                for (int j = 0; j < (1 << SHIFT) / 32; ++j) {
-                    const uint4 u = p[j * 4 + l];
-                    const __half *e = reinterpret_cast<const __half *>(&u);
-#pragma unroll
-                    for (int q = 0; q < 8; ++q) v += to_float(e[q]);
-                }
-                v += __shfl_xor_sync(0xffffffffu, v, 1);
-                v += __shfl_xor_sync(0xffffffffu, v, 2);
-                if (l == 0) xsum[i] = v;
-            }
-            consumers_meet();
-        }
-
         // this lane's column of each tile; a column that is not there reads another's, and its sums are not looked at
         const unsigned char *xl[NT];
 #pragma unroll
@@ -515,7 +497,6 @@ int4_matvec_kernel(const __grid_constant__ Int4Args a) {
             if (f0 + warp < records) {
                 const unsigned char *rec = smem + (stage * kPerStage + warp % kPerStage) * kRecord;
                 const int xo = c * kChunk * 2;
-                const float *xs_row = xsum + c * GC * COLS + 2 * t;
                 float part[NT][4];
 #pragma unroll
                 for (int p = 0; p < 4; ++p) {
@@ -535,19 +516,17 @@ int4_matvec_kernel(const __grid_constant__ Int4Args a) {
                         // rows r: 1024 + code; rows r + 8, four bits higher: 1024 + 16 code
                         const uint32_t up = word[s] >> 8;
                         uint32_t q[4] = {and_or(word[s], low, magic), and_or(word[s], high, magic), and_or(up, low, magic), and_or(up, high, magic)};
-                        if (kF32) {
-                            // code - zero and (1024 + 16 code) / 16 - (64 + zero), both exact
-                            uint32_t z0 = 0xe408e408u, z1 = 0xd480d480u;            // -1032, -72
-                            if (ZEROS) {
-                                const uint32_t zz = *reinterpret_cast<const unsigned short *>(rec + kZeroAt + (g * 8 + r) * 2);
-                                z0 = 0xe400e400u | ((zz & 15u) * 0x00010001u);
-                                z1 = 0xd400d400u | (((zz >> 8) & 15u) * 0x00100010u);
-                            }
-                            q[0] = fma2_half(q[0], 0x3c003c00u, z0);
-                            q[1] = fma2_half(q[1], 0x2c002c00u, z1);
-                            q[2] = fma2_half(q[2], 0x3c003c00u, z0);
-                            q[3] = fma2_half(q[3], 0x2c002c00u, z1);
+                        // code - zero and (1024 + 16 code) / 16 - (64 + zero), both exact
+                        uint32_t z0 = 0xe408e408u, z1 = 0xd480d480u;                // -1032, -72
+                        if (ZEROS) {
+                            const uint32_t zz = *reinterpret_cast<const unsigned short *>(rec + kZeroAt + (g * 8 + r) * 2);
+                            z0 = 0xe400e400u | ((zz & 15u) * 0x00010001u);
+                            z1 = 0xd400d400u | (((zz >> 8) & 15u) * 0x00100010u);
                         }
+                        q[0] = fma2_half(q[0], 0x3c003c00u, z0);
+                        q[1] = fma2_half(q[1], 0x2c002c00u, z1);
+                        q[2] = fma2_half(q[2], 0x3c003c00u, z0);
+                        q[3] = fma2_half(q[3], 0x2c002c00u, z1);
 #pragma unroll
                         for (int j = 0; j < NT; ++j) {
                             if (step % GSTEPS == 0) mma16816<true>(part[j], q, b[j][s >> 1][(s & 1) * 2], b[j][s >> 1][(s & 1) * 2 + 1]);
@@ -557,28 +536,10 @@ int4_matvec_kernel(const __grid_constant__ Int4Args a) {
                             const S2 v = *reinterpret_cast<const S2 *>(rec + (g * 8 + r) * sizeof(S2));
                             float s0, s1;
                             if constexpr (kF32) { s0 = v.x; s1 = v.y; }
+                            else if constexpr (kScaled) { s0 = __uint_as_float(v << 16); s1 = __uint_as_float(v & 0xffff0000u); }
                             else {
-                                float zl = 8.0f, zh = 8.0f;           // zero points of rows r and r + 8
-                                if (ZEROS) {
-                                    const uint32_t zz = *reinterpret_cast<const unsigned short *>(rec + kZeroAt + (g * 8 + r) * 2);
-                                    zl = (float)(zz & 255u);
-                                    zh = (float)(zz >> 8);
-                                }
-                                if constexpr (kScaled) { s0 = __uint_as_float(v << 16); s1 = __uint_as_float(v & 0xffff0000u); }
-                                else {
-                                    s0 = __half2float(__ushort_as_half((unsigned short)(v & 0xffffu)));
-                                    s1 = __half2float(__ushort_as_half((unsigned short)(v >> 16)));
-                                }
-                                const float k0 = -(1024.0f + zl), k1 = -(1024.0f + 16.0f * zh);
-                                s1 *= 0.0625f;
-#pragma unroll
-                                for (int j = 0; j < NT; ++j) {
-                                    const float2 xs = *reinterpret_cast<const float2 *>(xs_row + g * COLS + j * 8);
-                                    part[j][0] = fmaf(k0, xs.x, part[j][0]);
-                                    part[j][1] = fmaf(k0, xs.y, part[j][1]);
-                                    part[j][2] = fmaf(k1, xs.x, part[j][2]);
-                                    part[j][3] = fmaf(k1, xs.y, part[j][3]);
-                                }
+                                s0 = __half2float(__ushort_as_half((unsigned short)(v & 0xffffu)));
+                                s1 = __half2float(__ushort_as_half((unsigned short)(v >> 16)));
                             }
 #pragma unroll
                             for (int j = 0; j < NT; ++j) {
@@ -626,32 +587,30 @@ int4_matvec_kernel(const __grid_constant__ Int4Args a) {
 template <typename T, int NT, bool ZEROS, int SHIFT>
 cert_status_t launch_matvec3(const cert_int4 *op, Int4Args a, cudaStream_t st) {
     constexpr bool kF32 = std::is_same<T, float>::value;
-    constexpr int GC = kChunk >> SHIFT;
     const int stage_bytes = kPerStage * op->record;
     const int rows = a.rows_pass, cols = kF32 ? 2 * rows : rows;
     const int red = sums_bufs(NT) * kWarps * 20 * 8 * NT * 4;
     const int blocks = std::min(op->row_tiles, op->sms), items = (op->row_tiles + blocks - 1) / blocks;
     // the panel of x: all of K where it leaves two stages and half the memory, else equal parts
-    const int xsum_chunk = kF32 ? 0 : GC * 8 * NT * 4, x_chunk = cols * kChunk * 2;
+    const int x_chunk = cols * kChunk * 2;
     const long long outs = (long long)items * 16 * rows * 4;
     const int room = std::min(kSmemBlock - red - 4 * stage_bytes - 64 * cols - 128, kSmemBlock / 2);
-    int most = room / (x_chunk + xsum_chunk);
+    int most = room / x_chunk;
     a.panels = 1;
     if (most < a.chunks) {
-        most = room > outs ? (int)((room - outs) / (x_chunk + xsum_chunk)) : 0;
+        most = room > outs ? (int)((room - outs) / x_chunk) : 0;
         if (most < 1) return CERT_ERR_UNSUPPORTED;
         a.panels = (a.chunks + most - 1) / most;
     }
     a.panel_chunks = (a.chunks + a.panels - 1) / a.panels;
     a.panels = (a.chunks + a.panel_chunks - 1) / a.panel_chunks;
     a.x_pitch = a.panel_chunks * kChunk * 2 + 64;                     // eight lanes' 16 bytes: two columns, all banks
-    const int x_bytes = cols * a.x_pitch, xsum = a.panel_chunks * xsum_chunk, out_bytes = a.panels > 1 ? (int)outs : 0;
+    const int x_bytes = cols * a.x_pitch, out_bytes = a.panels > 1 ? (int)outs : 0;
     // an even number: a stage's place then belongs to one half of the warps, which have seen what was there before land
-    a.stages = std::min(kMaxStages, (kSmemBlock - 128 - red - x_bytes - xsum - out_bytes) / stage_bytes) & ~1;
+    a.stages = std::min(kMaxStages, (kSmemBlock - 128 - red - x_bytes - out_bytes) / stage_bytes) & ~1;
     a.red_off = (a.stages * stage_bytes + 127) / 128 * 128;
     a.x_off = a.red_off + red;
-    a.xsum_off = a.x_off + x_bytes;
-    a.out_off = a.xsum_off + xsum;
+    a.out_off = a.x_off + x_bytes;
     const int smem = a.out_off + out_bytes;
     auto kernel = int4_matvec_kernel<T, NT, ZEROS, SHIFT>;
     static bool allowed[64] = {};

@@ -5,7 +5,7 @@ import sys
 
 import pytest
 
-from test_gpu_operators import _xent_case, _xent_check
+from test_gpu_operators import TINY, U, _close, _gen, _int4_weights, _xent_case, _xent_check
 
 pytestmark = pytest.mark.gpu
 
@@ -77,3 +77,23 @@ def test_int4_weights_are_laid_out_when_the_constructor_returns(B):
     first = op.matvec(x)
     torch.cuda.synchronize()
     assert bool((op.matvec(x) == first).all()) and op.last_status() == 0
+
+
+@pytest.mark.parametrize("kind", ["float16", "bfloat16"])
+@pytest.mark.parametrize("group", [32, 64, 128, 256])
+@pytest.mark.parametrize("zeros", [False, True])
+def test_int4_inputs_of_one_sign(B, kind, group, zeros):
+    """Inputs as a ReLU leaves them, and constant ones: what an accumulator loses goes one way.  It holds sums of weights times x
+    and nothing larger: group / 16 products, truncated, then one addition per group, per warp and for the scale's power of two, all
+    relative to the sum of the products' magnitudes; bfloat16 x is off by 2^-40 of the row's largest value at most."""
+    import torch
+    for m, n, k in ((1, 512, 4096), (4, 512, 8192), (13, 500, 4096), (16, 100, 1000)):
+        codes, scales, zp, w = _int4_weights(kind, n, k, group, zeros, seed=group + m)
+        op = B.Int4Weight(codes, scales, k, group, zeros=zp)
+        for x in (torch.randn(m, k, generator=_gen(m), device="cuda").relu(), torch.full((m, k), 3.0, device="cuda")):
+            x = x.to(scales.dtype)
+            want, terms = x.double() @ w.t(), x.double() @ w.abs().t()
+            bound = terms * ((group / 16 + 2) * 2.0 ** -23 + (scales.shape[1] + 20) * 2.0 ** -24)
+            bound = bound + 2.0 ** -39 * x.double().amax(1, keepdim=True) * w.abs().sum(1)[None]
+            _close(op.matvec(x), want, 1.01 * bound + 1.01 * U[kind] * want.abs() + TINY[kind], "y")
+    assert op.last_status() == 0
