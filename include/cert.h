@@ -511,6 +511,7 @@ cert_status_t cert_clip_destroy(cert_clip_t *op);
  *            apart.  zeros == NULL: scale = max|w| / 7 of the group, code = round(w / scale) + 8; else scale =
  *            (max(w, 0) - min(w, 0)) / 15, zero = round(-min(w, 0) / scale), code = round(w / scale) + zero, clamped
  *            to 0 .. 15; rounding to nearest, ties to even, with the scale as rounded to `type`.
+ *            A group with a NaN or an infinity gets the scale NaN: its weights, and every product with them, are NaN.
  */
 typedef struct cert_int4 cert_int4_t;
 cert_status_t cert_int4_create(const unsigned char *codes, const void *scales, const unsigned char *zeros, int out_features,

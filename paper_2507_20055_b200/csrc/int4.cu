@@ -140,17 +140,21 @@ int4_quantize_kernel(const T *__restrict__ w, long long ldw, int N, int K, int g
     const int g = (int)(id - n * groups);
     const int k0 = g * group, k1 = min(K, k0 + group);
     float hi = 0.0f, lo = 0.0f;
+    bool finite = true;
     for (int k = k0 + lane; k < k1; k += 32) {
         const float v = to_float(w[n * ldw + k]);
         hi = fmaxf(hi, v);
         lo = fminf(lo, v);
+        finite = finite && fabsf(v) < INFINITY;
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
         hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
         lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
     }
-    const T st = from_float<T>(zeros ? (hi - lo) / 15.0f : fmaxf(hi, -lo) / 7.0f);
+    // no code stands for a NaN or an infinity: the scale does, so that the group's weights do not come back as ordinary numbers
+    finite = __all_sync(0xffffffffu, finite);
+    const T st = from_float<T>(!finite ? NAN : zeros ? (hi - lo) / 15.0f : fmaxf(hi, -lo) / 7.0f);
     const float s = to_float(st);
     const bool usable = s > 0.0f;
     const float z = zeros ? (usable ? fminf(fmaxf(rintf(-lo / s), 0.0f), 15.0f) : 0.0f) : 8.0f;

@@ -97,3 +97,25 @@ def test_int4_inputs_of_one_sign(B, kind, group, zeros):
             bound = bound + 2.0 ** -39 * x.double().amax(1, keepdim=True) * w.abs().sum(1)[None]
             _close(op.matvec(x), want, 1.01 * bound + 1.01 * U[kind] * want.abs() + TINY[kind], "y")
     assert op.last_status() == 0
+
+
+@pytest.mark.parametrize("kind", ["float32", "float16", "bfloat16"])
+@pytest.mark.parametrize("zeros", [False, True])
+def test_int4_quantize_hides_no_value_that_is_not_finite(B, kind, zeros):
+    import torch
+    w = (torch.randn(6, 200, generator=_gen(3), device="cuda") * 0.1).to(getattr(torch, kind))
+    want = B.int4_quantize(w, 64, zeros)
+    for bad in (float("nan"), float("inf"), -float("inf")):
+        v = w.clone()
+        v[1, 70], v[3, 199], v[5] = bad, bad, bad
+        codes, scales, zp = B.int4_quantize(v, 64, zeros)
+        hit = torch.zeros(6, 4, dtype=torch.bool, device="cuda")
+        hit[1, 1] = hit[3, 3] = True
+        hit[5] = True
+        assert bool(torch.isnan(scales[hit]).all()) and bool((scales[~hit] == want[1][~hit]).all())
+        back = B.Int4Weight(codes, scales, 200, 64, zeros=zp)
+        assert bool((torch.isnan(back.dequantize()) == hit.repeat_interleave(64, 1)[:, :200]).all())
+        kept = ~hit.repeat_interleave(64, 1)[:, :200:2]
+        assert bool((codes[kept] == want[0][kept]).all())
+        y = back.matvec(torch.ones(2, 200, device="cuda").to(w.dtype), relu=True)
+        assert bool((torch.isnan(y) == hit.any(1)[None]).all())
