@@ -601,19 +601,40 @@ class GradClipper:
 
     grads: contiguous CUDA tensors of float32, bfloat16 or float16, mixed as they come.  out: where the scaled ones go
     (same shapes and types; None: in place).  The list is laid out on the device once, here; clip() reads what the tensors
-    hold when it runs.  The object keeps references to both lists.
+    hold when it runs.  The object keeps both lists and their memory, so tensors have to stay the gradients' buffers: if backward
+    makes new ones (after zero_grad(set_to_none=True)), the old ones would be clipped.  A torch.nn.Parameter in the list
+    stands for its .grad, whichever that is when clip() runs (none: nothing to clip); a new one is laid out then, which allocates
+    and waits for the device, so kept buffers (set_to_none=False) are the quick way and the one for CUDA graphs.
     """
 
     def __init__(self, grads: Sequence, out: Optional[Sequence] = None, device=None):
         import torch
-        self.grads = list(grads)
-        self.out = self.grads if out is None else list(out)
-        self.device = _cuda_device(self.grads[0].device if device is None and self.grads else device)
-        if len(self.out) != len(self.grads):
-            raise ValueError(f"out: {len(self.out)} tensors for {len(self.grads)}")
-        arr = (cert_tensor_t * max(1, len(self.grads)))()
-        to = (_vp * max(1, len(self.grads)))()
-        for i, (t, o) in enumerate(zip(self.grads, self.out)):
+        self._given, self._to = list(grads), None if out is None else list(out)
+        self._h = None
+        self._follow = [i for i, t in enumerate(self._given) if isinstance(t, torch.nn.Parameter)]
+        self.device = _cuda_device(self._given[0].device if device is None and self._given else device)
+        if self._to is not None and len(self._to) != len(self._given):
+            raise ValueError(f"out: {len(self._to)} tensors for {len(self._given)}")
+        self._lay_out(self._current())
+        self._number = torch.empty((), dtype=torch.float32, device=self.device)
+
+    _follow = ()
+
+    def _current(self):
+        now = list(self._given)
+        for i in self._follow:
+            now[i] = now[i].grad
+        return now
+
+    def _lay_out(self, grads):
+        """The list of these gradients (None: no gradient) on the device, in place of the one that was there."""
+        import torch
+        out = grads if self._to is None else self._to
+        arr = (cert_tensor_t * max(1, len(grads)))()
+        to = (_vp * max(1, len(grads)))()
+        for i, (t, o) in enumerate(zip(grads, out)):
+            if t is None:
+                continue
             if not t.is_cuda or t.device != self.device or not t.is_contiguous():
                 raise ValueError(f"grads[{i}]: a contiguous tensor on {self.device} is required")
             if o.device != self.device or not o.is_contiguous() or o.dtype != t.dtype or o.shape != t.shape:
@@ -622,13 +643,19 @@ class GradClipper:
             to[i] = o.data_ptr() or None
         h = _vp()
         with torch.cuda.device(self.device):
-            _check(_lib.cert_clip_create(arr, len(self.grads), to, ctypes.byref(h)), "cert_clip_create")
-        self._h = h
-        self._number = torch.empty((), dtype=torch.float32, device=self.device)
+            _check(_lib.cert_clip_create(arr, len(grads), to, ctypes.byref(h)), "cert_clip_create")
+        self.destroy()
+        self._h, self.grads, self.out = h, grads, out
+        self._at = [t is not None and t.data_ptr() for t in grads]
+        self._memory = [t.untyped_storage() for t in (*grads, *out) if t is not None]       # whatever becomes of the tensors
 
     def clip(self, max_norm: float, norm_out=None, stream=None):
         """Scales the tensors into `out` and returns their norm before scaling (float32, on the device)."""
         import torch
+        if self._follow:
+            now = self._current()
+            if any(a is not b or a is not None and a.data_ptr() != at for a, b, at in zip(now, self.grads, self._at)):
+                self._lay_out(now)
         if norm_out is None:
             norm_out = _empty((), torch.float32, self.device, stream, self._number)
         elif norm_out.device != self.device or norm_out.dtype != torch.float32 or norm_out.numel() != 1:

@@ -119,3 +119,44 @@ def test_int4_quantize_hides_no_value_that_is_not_finite(B, kind, zeros):
         assert bool((codes[kept] == want[0][kept]).all())
         y = back.matvec(torch.ones(2, 200, device="cuda").to(w.dtype), relu=True)
         assert bool((torch.isnan(y) == hit.any(1)[None]).all())
+
+
+@pytest.mark.parametrize("in_place", [True, False])
+def test_clip_follows_the_gradients_of_parameters(B, in_place):
+    """With torch's default zero_grad the gradients are new tensors every step: parameters stand for the ones of the day."""
+    import math
+    import torch
+    torch.manual_seed(5)
+    params = [torch.nn.Parameter(torch.randn(s, device="cuda")) for s in ((300, 70), (70,), (5000,))]
+    params.append(torch.nn.Parameter(torch.randn(9, device="cuda").to(torch.bfloat16)))
+    unused = torch.nn.Parameter(torch.randn(11, device="cuda"))
+    plain = torch.randn(40, device="cuda")                 # a buffer among them stays what it is
+    out = None if in_place else [torch.full_like(p.data, 7.0) for p in (*params, unused)] + [torch.empty_like(plain)]
+    x, held, op = torch.randn(20, 300, device="cuda"), [], None
+    for step in range(4):
+        for p in params:
+            p.grad = None
+        held.append([torch.empty(1 << (8 + step), device="cuda")])            # so that addresses differ
+        ((x @ params[0] + params[1]).square().sum() + (step + 1) * params[2].sum() + params[3].float().square().sum()).backward()
+        held[-1] += [p.grad for p in params]
+        if op is None:
+            op = B.GradClipper([*params, unused, plain], out=out)
+        before = [p.grad.double() for p in params] + [plain.double()]
+        data = [p.detach().clone() for p in (*params, unused)]
+        norm = float(op.clip(1.0))
+        want = math.sqrt(sum(float((g ** 2).sum()) for g in before))
+        assert abs(norm - want) <= 2.0 ** -19 * want
+        got = [p.grad for p in params] + [plain] if in_place else [op.out[i] for i in (0, 1, 2, 3, 5)]
+        for g, o in zip(before, got):
+            kind = str(o.dtype).replace("torch.", "")
+            _close(o, g / (want + 1e-6), (g / (want + 1e-6)).abs() * (U[kind] + 2.0 ** -18) + TINY[kind], kind)
+        assert all(bool((a == b.detach()).all()) for a, b in zip(data, (*params, unused)))
+        if out is not None:
+            assert bool((out[4] == 7.0).all())
+        assert op.check_guards() == 0 and op.last_status() == 0
+    # kept buffers: the list stays
+    handle = op._h
+    for p in params:
+        p.grad.mul_(3.0)
+    op.clip(1.0)
+    assert op._h is handle
