@@ -95,14 +95,17 @@ private:
 };
 
 // Whether the device that a handle was made on is current: with another one, the default stream is that device's, and a launch
-// would get pointers of this one.
+// would get pointers of this one.  A host thread whose first call of CUDA this is has a current device but no context yet; a
+// launch would make one, encoding a tensor map needs it before that.
 inline bool on_device(int device) {
+    static thread_local int ready = -1;
     int current = -1;
-    if (cudaGetDevice(&current) != cudaSuccess) {
+    if (cudaGetDevice(&current) != cudaSuccess || current != device || (ready != device && cudaSetDevice(device) != cudaSuccess)) {
         cudaGetLastError();
         return false;
     }
-    return current == device;
+    ready = device;
+    return true;
 }
 
 // The status word of a handle as a return code; clears it.

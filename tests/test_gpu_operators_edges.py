@@ -160,3 +160,27 @@ def test_clip_follows_the_gradients_of_parameters(B, in_place):
         p.grad.mul_(3.0)
     op.clip(1.0)
     assert op._h is handle
+
+
+@pytest.mark.parametrize("kind", ["float32", "bfloat16"])
+def test_the_first_cuda_call_of_a_host_thread(B, kind):
+    """A new thread has no context before its first launch, and the tensor maps of a call are made before that."""
+    import threading
+    import torch
+    cases = [_xent_case(kind, rows, 256, 3000, True, 0.2, seed=rows) for rows in (500, 130)]
+    op = B.LinearCrossEntropy(500, 256, 3000, dtype=cases[0][0].dtype)
+    want = [[t.clone() for t in op.loss_and_grad(x, w, y, bias=b)] for x, w, y, b in cases]       # (and memory to hand out again)
+    torch.cuda.synchronize()
+    for (x, w, y, b), alone in zip(cases, want):
+        got = []
+
+        def call():
+            try:
+                got.extend(op.loss_and_grad(x, w, y, bias=b))
+            except Exception as e:
+                got.append(e)
+        thread = threading.Thread(target=call)
+        thread.start()
+        thread.join()
+        assert not isinstance(got[0], Exception), got[0]
+        assert all(bool((g == r).all()) for g, r in zip(got, alone))
