@@ -398,7 +398,8 @@ cert_status_t cert_peak_microbench(int kind, double target_ms, double *tflops_ou
  * unless marked HOST; work is enqueued on `stream` (a cudaStream_t, NULL = the default stream), the calls do not
  * wait and, after create, allocate nothing.  A handle belongs to the device that is current at its creation, and a
  * call with another device current is refused (CERT_ERR_INVALID_ARG); two calls on one handle must not overlap on the device
- * (they share its workspace).
+ * (they share its workspace).  Host threads may share a handle: a call waits until another thread's has put all of its work on
+ * its stream, so calls on one stream come one whole after the other.
  * ====================================================================================================== */
 
 /* Element types of the operators' matrices. */

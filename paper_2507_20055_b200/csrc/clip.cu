@@ -31,6 +31,7 @@ struct Piece {
 
 struct cert_clip {
     cert::OpBuffers mem;
+    std::mutex calls;
     int device = 0, sms = 1;
     int n_pieces = 0;
     cert::Piece *pieces = nullptr;
@@ -302,6 +303,8 @@ cert_status_t cert_clip_run(cert_clip_t *op, float max_norm, float *norm_out, vo
     using namespace cert;
     if (!op || !norm_out || !aligned(norm_out, 4) || !(max_norm >= 0.0f) || !on_device(op->device)) return CERT_ERR_INVALID_ARG;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const OpLock lock(op->calls);
+    if (!lock.held()) return CERT_ERR_CUDA;
 #ifdef CERT_BOUNDS
     {
         std::vector<OpBuffers::Out> outs = {{norm_out, 4}};

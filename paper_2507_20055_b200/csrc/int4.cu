@@ -16,6 +16,7 @@
 // the products, 21 us.  11009 x 4096 in groups of 64 with zero points, float16, 13 rows: 14.8 us (floor of the bytes 3.8), the
 // reads of x from shared memory, 16 columns for each record, and the five rounds of items being what is left.
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 #include <new>
 #include <type_traits>
@@ -617,7 +618,7 @@ cert_status_t launch_matvec3(const cert_int4 *op, Int4Args a, cudaStream_t st) {
     a.out_off = a.x_off + x_bytes;
     const int smem = a.out_off + out_bytes;
     auto kernel = int4_matvec_kernel<T, NT, ZEROS, SHIFT>;
-    static bool allowed[64] = {};
+    static std::atomic<bool> allowed[64] = {};
     if (!allowed[op->device & 63]) {
         if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBlock) != cudaSuccess) {
             cudaGetLastError();

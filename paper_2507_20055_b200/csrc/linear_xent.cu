@@ -24,6 +24,7 @@ struct cert_xent {
     bool with_grad = false;
     cert::XentSizes size = {};
     cert::OpBuffers mem;
+    std::mutex calls;
     int *status = nullptr;
     int *pos = nullptr, *idx = nullptr, *tgt = nullptr;   // row -> number among the kept ones (-1: ignored); back; class
     int *counts = nullptr;                                // [0] kept rows, [1] rows with a bad target, [2] ticket
@@ -787,6 +788,8 @@ cert_status_t cert_xent_run(cert_xent_t *op, const cert_xent_args_t *q, void *st
         return CERT_ERR_INVALID_ARG;
     if ((q->dx && q->lddx < op->size.D) || (q->dweight && q->lddw < op->size.D)) return CERT_ERR_INVALID_ARG;
     if ((q->dx || q->dweight || q->dbias) && !op->with_grad) return CERT_ERR_UNSUPPORTED;
+    const OpLock lock(op->calls);
+    if (!lock.held()) return CERT_ERR_CUDA;
 #ifdef CERT_BOUNDS
     {
         const size_t n = (size_t)q->rows, d = (size_t)op->size.D;

@@ -5,6 +5,7 @@
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
 #include <cstring>
+#include <mutex>
 #include <vector>
 
 #include "common.cuh"
@@ -107,6 +108,27 @@ inline bool on_device(int device) {
     ready = device;
     return true;
 }
+
+// One host thread at a time in a call on a handle: its launches stay together on the stream, and what the handle remembers of the
+// last call is one call's.
+class OpLock {
+public:
+    explicit OpLock(std::mutex &m) noexcept : m_(m) {
+        try {
+            m_.lock();
+            held_ = true;
+        } catch (...) {                      // no exception may reach the C ABI
+        }
+    }
+    ~OpLock() { if (held_) m_.unlock(); }
+    OpLock(const OpLock &) = delete;
+    OpLock &operator=(const OpLock &) = delete;
+    bool held() const { return held_; }
+
+private:
+    std::mutex &m_;
+    bool held_ = false;
+};
 
 // The status word of a handle as a return code; clears it.
 inline cert_status_t read_status(int *status_dev, cudaStream_t st) {

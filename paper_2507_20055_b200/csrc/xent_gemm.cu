@@ -16,6 +16,7 @@
 // turned, by the lanes): a thread holds a row, and 16 bytes of 32 different rows per store instruction cost the
 // epilogue more than its arithmetic (PROB, 919 x 50021 from 1000 features: 134 us stored by the threads, 87 without stores).
 #include <cuda.h>
+#include <atomic>
 
 #include "ops_common.cuh"
 #include "gemm_tc.cuh"
@@ -686,7 +687,7 @@ xent_gemm_kernel(const __grid_constant__ CUtensorMap map_a0, const __grid_consta
 typedef CUresult (*EncodeTiledXent)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
                                     const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
                                     CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-EncodeTiledXent g_encode = nullptr;
+std::atomic<EncodeTiledXent> g_encode{nullptr};
 
 template <int EPI, bool SUMS>
 void launch_one(int pairs, const XentMap &a0, const XentMap &b0, const XentMap &o0, const XentGemmArgs &g0, const XentMap &a1,
@@ -725,7 +726,7 @@ bool allow_smem() {
 }  // namespace
 
 bool xent_gemm_prepare() {
-    if (!g_encode) {
+    if (!g_encode.load()) {
         void *fn = nullptr;
         cudaDriverEntryPointQueryResult qres;
         if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &qres) != cudaSuccess ||
@@ -745,12 +746,13 @@ bool xent_gemm_prepare() {
 
 bool xent_make_map(XentMap *m, const void *base, bool bf16, long long inner, long long outer, long long pitch_elems,
                    int box_inner, int box_outer) {
-    if (!g_encode) return false;
+    const EncodeTiledXent encode = g_encode.load();
+    if (!encode) return false;
     cuuint64_t dims[2] = {(cuuint64_t)inner, (cuuint64_t)outer};
     cuuint64_t strides[1] = {(cuuint64_t)pitch_elems * 2};
     cuuint32_t box[2] = {(cuuint32_t)box_inner, (cuuint32_t)box_outer};
     cuuint32_t estr[2] = {1u, 1u};
-    return g_encode(reinterpret_cast<CUtensorMap *>(m), bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16,
+    return encode(reinterpret_cast<CUtensorMap *>(m), bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16,
                     2, const_cast<void *>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
                     CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                     CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
@@ -758,14 +760,15 @@ bool xent_make_map(XentMap *m, const void *base, bool bf16, long long inner, lon
 
 bool xent_make_out_map(XentMap *m, const void *base, int type, long long inner, long long outer, long long pitch_elems) {
     const int es = type_size(type);
-    if (!g_encode || !aligned(base, 16) || (pitch_elems * es) % 16 != 0 || pitch_elems * es >= (1LL << 40)) return false;
+    const EncodeTiledXent encode = g_encode.load();
+    if (!encode || !aligned(base, 16) || (pitch_elems * es) % 16 != 0 || pitch_elems * es >= (1LL << 40)) return false;
     cuuint64_t dims[2] = {(cuuint64_t)inner, (cuuint64_t)outer};
     cuuint64_t strides[1] = {(cuuint64_t)(pitch_elems * es)};
     cuuint32_t box[2] = {32, 32};
     cuuint32_t estr[2] = {1u, 1u};
     const CUtensorMapDataType t = type == CERT_TYPE_F32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
                                 : type == CERT_TYPE_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
-    return g_encode(reinterpret_cast<CUtensorMap *>(m), t, 2, const_cast<void *>(base), dims, strides, box, estr,
+    return encode(reinterpret_cast<CUtensorMap *>(m), t, 2, const_cast<void *>(base), dims, strides, box, estr,
                     CU_TENSOR_MAP_INTERLEAVE_NONE, type == CERT_TYPE_F32 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
                     CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }

@@ -184,3 +184,34 @@ def test_the_first_cuda_call_of_a_host_thread(B, kind):
         thread.join()
         assert not isinstance(got[0], Exception), got[0]
         assert all(bool((g == r).all()) for g, r in zip(got, alone))
+
+
+def test_host_threads_share_a_handle_on_one_stream(B):
+    """Two threads call one object with different sizes: every result is the one of the call alone, to the bit."""
+    import threading
+    import torch
+    cases = [_xent_case("bfloat16", rows, 256, 3000, True, 0.2, seed=rows) for rows in (500, 130)]
+    op = B.LinearCrossEntropy(500, 256, 3000, dtype=torch.bfloat16)
+    alone = [[t.clone() for t in op.loss_and_grad(x, w, y, bias=b)] for x, w, y, b in cases]
+    grads = [torch.randn(n, generator=_gen(n), device="cuda") for n in (100000, 77, 3000)]
+    clip = B.GradClipper(grads, out=[torch.empty_like(t) for t in grads])
+    norm = float(clip.clip(1.0))
+    torch.cuda.synchronize()
+    wrong, stream = [], torch.cuda.current_stream()
+
+    def calls(i):
+        try:
+            with torch.cuda.stream(stream):
+                for _ in range(200):
+                    x, w, y, b = cases[i]
+                    got = op.loss_and_grad(x, w, y, bias=b)
+                    if not all(bool((g == r).all()) for g, r in zip(got, alone[i])) or float(clip.clip(1.0)) != norm:
+                        wrong.append(i)
+        except Exception as e:
+            wrong.append(e)
+    threads = [threading.Thread(target=calls, args=(i,)) for i in (0, 1)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert wrong == [] and op.last_status() == 0 and op.check_guards() == 0 and clip.check_guards() == 0

@@ -98,3 +98,11 @@ def test_c_calls_on_a_handle_ask_for_its_device():
         for call, body in calls:
             first_use = min(body.index(w) for w in ("op->mem", "op->status", "cudaDeviceSynchronize", "run(op", "static_cast<cudaStream_t>") if w in body)
             assert "on_device(op->device)" in body[:first_use], call
+
+
+def test_calls_that_use_a_handles_workspace_are_taken_one_at_a_time():
+    """Two host threads on one stream: what the handle remembers and the order of the launches are one call's at a time."""
+    for name, call, work in (("linear_xent.cu", "cert_xent_run", "return run("), ("clip.cu", "cert_clip_run", "launch_chained(")):
+        with open(os.path.join(ROOT, "paper_2507_20055_b200", "csrc", name)) as f:
+            body = f.read().split(f"cert_status_t {call}(")[1].split("\n}\n")[0]
+        assert "const OpLock lock(op->calls);" in body[:body.index(work)]
