@@ -41,6 +41,16 @@ constexpr int kMaxStages = 12;
 // values around zero and 5e-7 to 4e-6 for positive ones.  64 rows, 65536 classes, 4096 features, loss alone: 114.7 us
 // against 124.0 with 512 terms; 4096 rows, 32768 classes, 2048 features, with gradients: 1.62 ms against 1.69.
 constexpr int kSumBlocks32 = 8, kSumBlocks16 = 16;
+// Gradient products of 16-bit operands are rounded to that type, which hides the bias of a short accumulator and not of a long one:
+// for terms of one sign it is some 1.2e-7 to 2.3e-7 per 16 of them.  So K beyond 4096 terms (float16; its rounding's root mean
+// square is 2.1e-4) or 32768 (bfloat16, 1.7e-3) goes into accumulators of 4096 terms: the bias stays at 6e-5.
+// float16, 262144 rows behind a ReLU, 512 features, 8192 classes: dW 9.7e-4 off, relative, in one accumulator, 2.9e-4 so, its
+// rounding alone 2.1e-4; 1531 x 1000 x 50021 with 40 % ignored: 449-458 us against 434-440.
+constexpr int kSumBlocksStore = 64;
+constexpr int kStoreTermsHalf = 4096, kStoreTermsBf16 = 32768;
+// Probabilities take their logits' error times the logit; with more features than this their logits are added up as the losses'
+// are, to the same bits.  (Always: 1531 x 1000 x 50021 487 us against 437.)
+constexpr int kProbTermsHalf = 1024, kProbTermsBf16 = 4096;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
@@ -163,7 +173,7 @@ __device__ __forceinline__ Tile tile_of(int t, int tiles_m, int tiles_n, int ras
 // What a launch has to do for one product.
 struct Shape { int M, tiles_m, tiles_n, num_kb, kb_per, sum_blocks, total; };
 
-template <bool SUMS>
+template <int EPI, bool SUMS>
 __device__ __forceinline__ Shape shape_of(const XentGemmArgs &a) {
     Shape s;
     s.M = a.m_count ? min(a.M, *a.m_count) : a.M;
@@ -174,7 +184,8 @@ __device__ __forceinline__ Shape shape_of(const XentGemmArgs &a) {
     const int splits = a.most_splits > 1 ? xent_splits(s.tiles_m * s.tiles_n, a.split_kb ? a.split_kb : s.num_kb, a.segs, a.pairs, a.most_splits) : 1;
     s.kb_per = (s.num_kb + splits - 1) / splits;
     s.total = s.tiles_m * s.tiles_n * splits;
-    s.sum_blocks = SUMS ? (a.segs > 1 ? kSumBlocks32 : kSumBlocks16) : max(1, s.kb_per);       // K blocks per accumulator
+    // K blocks per accumulator
+    s.sum_blocks = !SUMS ? max(1, s.kb_per) : a.segs > 1 ? kSumBlocks32 : EPI == XENT_EPI_STORE ? kSumBlocksStore : kSumBlocks16;
     return s;
 }
 
@@ -228,7 +239,7 @@ xent_gemm_kernel(const __grid_constant__ CUtensorMap map_a0, const __grid_consta
     const uint32_t tmem_base = bars->tmem_base;
     volatile uint32_t *abort_flag = &bars->abort_flag;
 
-    const Shape s0 = shape_of<SUMS>(g0), s1 = kStore ? shape_of<SUMS>(g1) : Shape{};
+    const Shape s0 = shape_of<EPI, SUMS>(g0), s1 = kStore ? shape_of<EPI, SUMS>(g1) : Shape{};
     const int total = s0.total + (kStore ? s1.total : 0);
 
     const uint32_t smem0 = smem_u32(smem), full0 = smem_u32(&bars->full[0]), empty0 = smem_u32(&bars->empty[0]);
@@ -774,15 +785,16 @@ bool xent_make_out_map(XentMap *m, const void *base, int type, long long inner, 
 }
 
 void launch_xent_gemm(int epi, int pairs, const XentMap &a, const XentMap &b, const XentMap &out, const XentGemmArgs &args, cudaStream_t st) {
-    // sums in registers for the loss, and for everything in float32; a 16-bit result's rounding hides the bias
+    // sums in registers for the loss, for everything in float32, and for long sums
     if (epi == XENT_EPI_LSE) launch_one<XENT_EPI_LSE, true>(pairs, a, b, a, args, a, b, a, args, st);
     else if (epi == XENT_EPI_ROW) launch_one<XENT_EPI_ROW, true>(pairs, a, b, out, args, a, b, out, args, st);
-    else if (args.segs > 1) launch_one<XENT_EPI_PROB, true>(pairs, a, b, out, args, a, b, out, args, st);
+    else if (args.segs > 1 || args.K > (args.bf16 ? kProbTermsBf16 : kProbTermsHalf)) launch_one<XENT_EPI_PROB, true>(pairs, a, b, out, args, a, b, out, args, st);
     else launch_one<XENT_EPI_PROB, false>(pairs, a, b, out, args, a, b, out, args, st);
 }
 
 void launch_xent_store(int pairs, const XentProduct &p, const XentProduct &q, cudaStream_t st) {
-    if (p.args.segs > 1) launch_one<XENT_EPI_STORE, true>(pairs, p.a, p.b, p.out, p.args, q.a, q.b, q.out, q.args, st);
+    const int K = q.args.N && q.args.K > p.args.K ? q.args.K : p.args.K;       // (the device may cut it into ranges, or not)
+    if (p.args.segs > 1 || K > (p.args.bf16 ? kStoreTermsBf16 : kStoreTermsHalf)) launch_one<XENT_EPI_STORE, true>(pairs, p.a, p.b, p.out, p.args, q.a, q.b, q.out, q.args, st);
     else launch_one<XENT_EPI_STORE, false>(pairs, p.a, p.b, p.out, p.args, q.a, q.b, q.out, q.args, st);
 }
 

@@ -215,3 +215,53 @@ def test_host_threads_share_a_handle_on_one_stream(B):
     for t in threads:
         t.join()
     assert wrong == [] and op.last_status() == 0 and op.check_guards() == 0 and clip.check_guards() == 0
+
+
+def _rounded_dz(x, w, y):
+    """float64 probabilities minus one at the target, rounded to the type as the gradient products get them (float16: times 2^14)."""
+    import torch
+    p = torch.softmax(x.double() @ w.double().t(), 1)
+    p[torch.arange(len(y), device="cuda"), y] -= 1
+    scale = 2.0 ** 14 if x.dtype == torch.float16 else 1.0
+    return (p * scale).to(x.dtype).double() / scale
+
+
+# accumulators of at most 4096 terms, 256 products of 16, each truncated by at most 2^-23 of what is there
+LONG_SUMS = 256 * 2.0 ** -23
+
+
+@pytest.mark.parametrize("kind", ["float16", "bfloat16"])
+def test_xent_many_rows_of_one_sign(B, kind):
+    """dW over 262144 rows of inputs behind a ReLU: truncation goes one way, so it must show in the mean error no more than
+    accumulators of a bounded length let it (the roundings of the result are as often up as down)."""
+    import torch
+    rows, features, classes = 262144, 512, 8192
+    x = torch.randn(rows, features, generator=_gen(1), device="cuda").relu().to(getattr(torch, kind))
+    w = (torch.randn(classes, features, generator=_gen(2), device="cuda") / features ** 0.5).to(x.dtype)
+    y = torch.randint(0, classes, (rows,), generator=_gen(3), device="cuda")
+    op = B.LinearCrossEntropy(rows, features, classes, dtype=x.dtype)
+    dw = op.loss_and_grad(x, w, y, reduction="sum")[2].double()
+    assert op.last_status() == 0 and op.check_guards() == 0
+    want, terms = torch.zeros_like(dw), torch.zeros_like(dw)
+    for a in range(0, rows, 8192):
+        dz, xs = _rounded_dz(x[a:a + 8192], w, y[a:a + 8192]), x[a:a + 8192].double()
+        want += dz.t() @ xs
+        terms += dz.abs().t() @ xs
+    assert abs(float((dw - want).mean())) <= LONG_SUMS * float(terms.mean())
+
+
+@pytest.mark.parametrize("kind,features", [("float16", 16384), ("bfloat16", 32768)])
+def test_xent_many_features_of_one_sign(B, kind, features):
+    """Inputs and weights that are all positive: the probabilities' logits are the losses', whose accumulators have 1024 terms."""
+    import torch
+    rows, classes = 512, 4096
+    x = torch.randn(rows, features, generator=_gen(1), device="cuda").relu().to(getattr(torch, kind))
+    w = (torch.rand(classes, features, generator=_gen(2), device="cuda") * (100.0 / features)).to(x.dtype)
+    y = torch.randint(0, classes, (rows,), generator=_gen(3), device="cuda")
+    op = B.LinearCrossEntropy(rows, features, classes, dtype=x.dtype)
+    dx = op.loss_and_grad(x, w, y, reduction="sum")[1].double()
+    assert op.last_status() == 0 and op.check_guards() == 0
+    dz = _rounded_dz(x, w, y)
+    logit = float((x.double() @ w.double().t()).max()) * (64 * 2.0 ** -23 + features / 1024 * 2.0 ** -24)
+    bound = (2 * logit + LONG_SUMS) * float((dz.abs() @ w.double()).mean())
+    assert abs(float((dx - dz @ w.double()).mean())) <= bound
