@@ -423,6 +423,8 @@ enum { CERT_TYPE_F32 = 0, CERT_TYPE_BF16 = 1, CERT_TYPE_F16 = 2 };
  *   or NULL: all of the handle's type; rows 0 .. max_rows.  target [rows] int32 or int64.
  *   A class with bias -infinity takes no part (probability 0, zero gradient; a target there gives loss +infinity); its
  *   weights have to be finite numbers all the same, since zero times them is summed.
+ *   A type's lowest value is such a mask too while another class is left, and swallows the logits where none is: all of
+ *   those classes are then as likely as one another.  Beyond 16 classes a finite bias counts as 2^127 in magnitude at most.
  *   An ignored row costs nothing and its x is never read; its dx is zero.  No row left: loss 0, zero gradients.
  *   A target outside [0, classes) that is not ignore_index: the row's loss and the loss are NaN, its gradient is
  *   zero, and cert_xent_last_status returns CERT_ERR_INVALID_ARG.

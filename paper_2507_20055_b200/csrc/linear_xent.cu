@@ -155,6 +155,14 @@ __device__ __forceinline__ void zero8(const BeginArgs &a, int row, int d) {
     for (int e = d; e < min(d + 8, a.D); ++e) store_from_float(a.dx_zero, (long long)row * a.lddx + e, a.bias_type, 0.0f);
 }
 
+// A bias as the kernels use it: a type's lowest value as a mask would leave the fp32 range times log2 e, and a row with nothing else
+// would have no finite maximum.
+__device__ __forceinline__ float usable_bias(float b) {
+    constexpr float kMost = 1.7014118346046923e38f;        // 2^127
+    if (b < -kMost && b > -INFINITY) return -kMost;
+    return b > kMost && b < INFINITY ? kMost : b;
+}
+
 // Start of a call.  A block takes consecutive rows (and, in grids of two dimensions, a share of their columns): it counts the rows before them that count, numbers its own in order and
 // copies them to their places in the padded x.  The last block knows the total; it clears the rows up to the next multiple
 // of 64, so that a block of K that reaches over the end adds nothing.  The bias becomes float32 on the way.
@@ -182,7 +190,7 @@ xent_begin_kernel(const T *__restrict__ x, const BeginArgs a) {
     wrong = block_count(wrong, scratch);
     if (a.bias && blockIdx.y == 0)
         for (int i = blockIdx.x * 256 + tid; i < a.Vp; i += gridDim.x * 256)
-            CERT_ST(a.bias32[i], i < a.classes ? load_as_float(a.bias, i, a.bias_type) : 0.0f);
+            CERT_ST(a.bias32[i], i < a.classes ? usable_bias(load_as_float(a.bias, i, a.bias_type)) : 0.0f);
     const int per = a.Dp / 8;
     for (int r0 = first; r0 < end; r0 += 256) {
         const int r = r0 + tid;

@@ -265,3 +265,34 @@ def test_xent_many_features_of_one_sign(B, kind, features):
     logit = float((x.double() @ w.double().t()).max()) * (64 * 2.0 ** -23 + features / 1024 * 2.0 ** -24)
     bound = (2 * logit + LONG_SUMS) * float((dz.abs() @ w.double()).mean())
     assert abs(float((dx - dz @ w.double()).mean())) <= bound
+
+
+@pytest.mark.parametrize("kind", ["float32", "bfloat16", "float16"])
+@pytest.mark.parametrize("classes", [10, 40, 200, 700])
+def test_xent_every_class_masked_by_the_lowest_value(B, kind, classes):
+    """The type's lowest value as a mask in every class swallows the logits: equal ones, so every class has the same probability,
+    whichever path the number of classes takes.  -infinity beside it leaves the others equal."""
+    import math
+    import torch
+    x, w, y, b = _xent_case(kind, 70, 64, classes, True, 0.0, seed=classes)
+    if kind == "float16":                                  # (-65504 swallows no logit in float32)
+        x = x * 0
+    low = torch.full_like(b, torch.finfo(b.dtype).min)
+    op = B.LinearCrossEntropy(70, 64, classes, dtype=x.dtype)
+    for gone in (0, classes // 2):
+        low[classes - gone:] = -float("inf")
+        y = y % (classes - gone)
+        loss, dx, dw, db = op.loss_and_grad(x, w, y, bias=low)
+        # 2^x, the sum and the logarithm as in the other tests
+        assert abs(float(loss) - math.log(classes - gone)) <= 2.0 ** -19 * (1 + math.log(classes))
+        p = torch.zeros(70, classes, dtype=torch.float64, device="cuda")
+        p[:, :classes - gone] = 1.0 / (classes - gone)
+        p[torch.arange(70, device="cuda"), y] -= 1
+        ep = p.abs() * (U[kind] + 2.0 ** -18) + (2.0 ** -38 if kind == "float16" else 0.0)
+        want = p.sum(0) / 70
+        _close(db, want, 1.01 * ep.sum(0) / 70 + 2 * U[kind] * want.abs() + 2.0 ** -20 * p.abs().sum(0) / 70 + TINY[kind], "db")
+        want, terms = p.t() @ x.double() / 70, p.abs().t() @ x.double().abs() / 70
+        _close(dw, want, 1.01 * ep.t() @ x.double().abs() / 70 + 2.0 ** -18 * terms + 2 * U[kind] * want.abs() + TINY[kind], "dw")
+        want, terms = p @ w.double() / 70, p.abs() @ w.double().abs() / 70
+        _close(dx, want, 1.01 * ep @ w.double().abs() / 70 + 2.0 ** -16 * terms + 2 * U[kind] * want.abs() + TINY[kind], "dx")
+    assert op.last_status() == 0 and op.check_guards() == 0
