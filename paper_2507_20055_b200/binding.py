@@ -428,6 +428,14 @@ def _type_code(dtype):
     return codes[dtype]
 
 
+def _int32(name, value):
+    """A size as the C ABI takes it: ctypes would cut off what an int does not hold."""
+    value = int(value)
+    if not -2 ** 31 <= value < 2 ** 31:
+        raise ValueError(f"{name}: {value} does not fit an int")
+    return value
+
+
 def _check_rows(name, t, shape, dtype, device):
     """A matrix whose rows may be any distance apart, the elements of a row next to each other."""
     if t.dtype is dtype and t.shape == shape and t.is_contiguous() and t.device == device:
@@ -510,12 +518,13 @@ class LinearCrossEntropy:
         import torch
         self.dtype = torch.float32 if dtype is None else dtype
         self.device = _cuda_device(device)
+        self.max_rows, self.features, self.classes = _int32("max_rows", max_rows), _int32("features", features), _int32("classes", classes)
+        self.grad = bool(grad)
         h = _vp()
         with torch.cuda.device(self.device):
-            _check(_lib.cert_xent_create(int(max_rows), int(features), int(classes), _type_code(self.dtype), int(bool(grad)),
+            _check(_lib.cert_xent_create(self.max_rows, self.features, self.classes, _type_code(self.dtype), int(self.grad),
                                          ctypes.byref(h)), "cert_xent_create")
         self._h = h
-        self.max_rows, self.features, self.classes, self.grad = int(max_rows), int(features), int(classes), bool(grad)
         self._number = torch.empty((), dtype=torch.float32, device=self.device)
         self._weight_shape, self._bias_shape = torch.Size((self.classes, self.features)), torch.Size((self.classes,))
 
@@ -532,7 +541,7 @@ class LinearCrossEntropy:
             _check_rows("bias", bias, self._bias_shape, dtype, device)
         if reduction != "mean" and reduction != "sum":
             raise ValueError(f"reduction {reduction!r}: 'mean' or 'sum' is required")
-        return cert_xent_args_t(rows, target.dtype is torch.int64, reduction == "sum", grad_scale, ignore_index,
+        return cert_xent_args_t(_int32("rows", rows), target.dtype is torch.int64, reduction == "sum", grad_scale, ignore_index,
                                 x.data_ptr(), _ld(x), weight.data_ptr(), _ld(weight),
                                 None if bias is None else bias.data_ptr(), target.data_ptr())
 
@@ -687,13 +696,13 @@ def int4_quantize(weight, group: int = 64, zeros: bool = False, stream=None):
     if weight.dim() != 2:
         raise ValueError("weight: a matrix is required")
     _check_rows("weight", weight, weight.shape, weight.dtype, weight.device)
-    n, k = weight.shape
+    n, k, group = _int32("rows", weight.shape[0]), _int32("columns", weight.shape[1]), _int32("group", group)
     groups = -(-k // group) if group > 0 else 0
     codes = _empty((n, (k + 1) // 2), torch.uint8, weight.device, stream)
     scales = _empty((n, groups), weight.dtype, weight.device, stream)
     zp = _empty((n, groups), torch.uint8, weight.device, stream) if zeros else None
     with torch.cuda.device(weight.device):
-        _check(_lib.cert_int4_quantize(weight.data_ptr(), _ld(weight), n, k, int(group), _type_code(weight.dtype), codes.data_ptr(),
+        _check(_lib.cert_int4_quantize(weight.data_ptr(), _ld(weight), n, k, group, _type_code(weight.dtype), codes.data_ptr(),
                                        scales.data_ptr(), zp.data_ptr() if zeros else None, _stream_ptr(stream, weight.device)),
                "cert_int4_quantize")
     return codes, scales, zp
@@ -709,10 +718,10 @@ class Int4Weight:
     def __init__(self, codes, scales, in_features: int, group: int, zeros=None, stream=None):
         import torch
         self.dtype, self.device = scales.dtype, scales.device
-        self.in_features, self.group = int(in_features), int(group)
+        self.in_features, self.group = _int32("in_features", in_features), _int32("group", group)
         if codes.dim() != 2 or self.group < 1:
             raise ValueError("codes: a matrix, and a positive group, are required")
-        self.out_features = int(codes.shape[0])
+        self.out_features = _int32("out_features", codes.shape[0])
         groups = -(-self.in_features // self.group)
         for name, t, shape, dtype in (("codes", codes, (self.out_features, (self.in_features + 1) // 2), torch.uint8),
                                       ("scales", scales, (self.out_features, groups), self.dtype),
@@ -745,7 +754,7 @@ class Int4Weight:
             out = _empty((rows, self.out_features), self.dtype, self.device, stream)
         else:
             _check_rows("out", out, (rows, self.out_features), self.dtype, self.device)
-        _check(_call(self.device, _lib.cert_int4_matvec, self._h, x.data_ptr(), _ld(x), rows, bias.data_ptr() if bias is not None else None,
+        _check(_call(self.device, _lib.cert_int4_matvec, self._h, x.data_ptr(), _ld(x), _int32("rows", rows), bias.data_ptr() if bias is not None else None,
                                      int(bool(relu)), out.data_ptr(), _ld(out), _stream_ptr(stream, self.device)),
                "cert_int4_matvec")
         return out

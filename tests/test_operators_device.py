@@ -106,3 +106,25 @@ def test_calls_that_use_a_handles_workspace_are_taken_one_at_a_time():
         with open(os.path.join(ROOT, "paper_2507_20055_b200", "csrc", name)) as f:
             body = f.read().split(f"cert_status_t {call}(")[1].split("\n}\n")[0]
         assert "const OpLock lock(op->calls);" in body[:body.index(work)]
+
+
+def test_sizes_that_an_int_does_not_hold_are_refused(fake):
+    """They would arrive cut to 32 bits: a layer of 2^32 + 3 outputs as one of 3, whose others nobody writes."""
+    import torch
+    binding, _, lib = fake
+    meta, many = torch.device("meta"), 2 ** 32 + 3
+    xent, layer = binding.LinearCrossEntropy.__new__(binding.LinearCrossEntropy), binding.Int4Weight.__new__(binding.Int4Weight)
+    for op in (xent, layer):
+        op._h, op.device, op.dtype = 1, torch.device("cuda", 0), torch.float32
+    xent.features, xent.classes, xent._weight_shape = 1, 20, torch.Size((20, 1))
+    layer.in_features, layer.out_features = 1, 20
+    x, w, y = torch.empty(many, 1, device=meta), torch.empty(20, 1, device=meta), torch.empty(many, dtype=torch.int64, device=meta)
+    codes, scales = torch.empty(many, 1, dtype=torch.uint8, device=meta), torch.empty(many, 1, device=meta)
+    for call in (lambda: xent.loss(x, w, y), lambda: xent.loss_and_grad(x, w, y), lambda: layer.matvec(x, out=x),
+                 lambda: binding.int4_quantize(x, 32), lambda: binding.Int4Weight(codes, scales, 1, 32),
+                 lambda: binding.Int4Weight(codes[:20], scales[:20], 1, many), lambda: binding.int4_quantize(w, many),
+                 lambda: binding.LinearCrossEntropy(many, 1, 20, device=torch.device("cuda", 0)),
+                 lambda: binding.LinearCrossEntropy(1, 1, many, device=torch.device("cuda", 0))):
+        with pytest.raises(ValueError, match="does not fit"):
+            call()
+    assert lib.seen == []
