@@ -45,11 +45,11 @@ constexpr int kSumBlocks32 = 8, kSumBlocks16 = 16;
 // for terms of one sign it is some 1.2e-7 to 2.3e-7 per 16 of them.  So K beyond 4096 terms (float16; its rounding's root mean
 // square is 2.1e-4) or 32768 (bfloat16, 1.7e-3) goes into accumulators of 4096 terms: the bias stays at 6e-5.
 // float16, 262144 rows behind a ReLU, 512 features, 8192 classes: dW 9.7e-4 off, relative, in one accumulator, 2.9e-4 so, its
-// rounding alone 2.1e-4; 1531 x 1000 x 50021 with 40 % ignored: 449-458 us against 434-440.
+// rounding alone 2.1e-4; 1531 x 1000 x 50021 with 40 % ignored: 454 us against 448.
 constexpr int kSumBlocksStore = 64;
 constexpr int kStoreTermsHalf = 4096, kStoreTermsBf16 = 32768;
 // Probabilities take their logits' error times the logit; with more features than this their logits are added up as the losses'
-// are, to the same bits.  (Always: 1531 x 1000 x 50021 487 us against 437.)
+// are, to the same bits.  (Always: 1531 x 1000 x 50021 483 us against 455.)
 constexpr int kProbTermsHalf = 1024, kProbTermsBf16 = 4096;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
@@ -77,6 +77,17 @@ __device__ __forceinline__ void select_if(float &to, float from, int at, int e) 
 }
 __device__ __forceinline__ void minus_if(float &x, float y, int at, int e) {
     asm("{\n\t.reg .pred p;\n\tsetp.eq.s32 p, %2, %3;\n\t@p sub.f32 %0, %0, %1;\n\t}" : "+f"(x) : "f"(y), "r"(at), "r"(e));
+}
+
+// Half of what tmem_ld32 reads: beside 128 sums a thread has no room for 32 more values (1531 x 1000 x 50021, float16: 443 us
+// against 463 with 32, 64 x 65536: 122 against 124, 1024 x 1024 x 8192 float32: 368 against 375).
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&v)[16]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]), "=r"(v[9]),
+          "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+        : "r"(taddr)
+        : "memory");
 }
 
 template <int PENDING>
@@ -400,12 +411,15 @@ xent_gemm_kernel(const __grid_constant__ CUtensorMap map_a0, const __grid_consta
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         if (c_begin + i < c_end) {
-                            uint32_t v[32];
-                            __syncwarp();
-                            tmem_ld32(t_addr + (uint32_t)(i * 32), v);
-                            tmem_ld_wait();
 #pragma unroll
-                            for (int e = 0; e < 32; ++e) sum[SUMS ? i : 0][e] += __uint_as_float(v[e]);
+                            for (int h = 0; h < 32; h += 16) {
+                                uint32_t v[16];
+                                __syncwarp();
+                                tmem_ld16(t_addr + (uint32_t)(i * 32 + h), v);
+                                tmem_ld_wait();
+#pragma unroll
+                                for (int e = 0; e < 16; ++e) sum[SUMS ? i : 0][h + e] += __uint_as_float(v[e]);
+                            }
                         }
                     }
                     tcgen05_fence_before();
