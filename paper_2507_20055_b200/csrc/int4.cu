@@ -12,9 +12,9 @@
 // x goes in as float16 times a power of two per row, which puts the row's largest value below 2^15: a bfloat16's eight bits stay
 // exact down to 2^-29 of the largest and are off by at most 2^-40 of it below; a float32 takes two columns, hi and lo, 22 bits.
 // A group's sum is multiplied by its scale in fp32; the warps' sums are added in a fixed order.
-// Measured: 28672 x 8192 in groups of 128, bfloat16, one row of x: 29.1 us, 121 MB of records at 4.2 TB/s; the copies alone, without
-// the products, 21 us.  11009 x 4096 in groups of 64 with zero points, float16, 13 rows: 14.8 us (floor of the bytes 3.8), the
-// reads of x from shared memory, 16 columns for each record, and the five rounds of items being what is left.
+// Measured: 28672 x 8192 in groups of 128, bfloat16, one row of x: 28.5 to 29.7 us over three cards, 121 MB of records at 4.1-4.2 TB/s;
+// the copies alone, without the products, 21 us.  11009 x 4096 in groups of 64 with zero points, float16, 13 rows: 14.2 us (floor of the bytes 3.8),
+// the reads of x from shared memory, 16 columns for each record, and the five rounds of items being what is left.
 #include <algorithm>
 #include <atomic>
 #include <cmath>

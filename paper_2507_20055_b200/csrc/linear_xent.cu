@@ -11,6 +11,9 @@
 // With up to 256 classes a tile holds whole rows, and one product (ROW) takes the place of LSE, combine and PROB.
 // With up to 16 classes and not too many rows all of it is two launches of another kind (xent_few.cu).
 // 2TVD operations for the loss, 8TVD with gradients; the probabilities of a piece stay below kProbBytes.
+// Sizes and cuts are worked out in xent_plan.cuh.  16-bit probabilities are a choice: both gradient products take them as
+// operands, and a second part would make 12TVD of the 8.  bfloat16 gradients are 1.9e-3 off, relative, where their own rounding is
+// 1.7e-3 (4096 x 2048 x 32768), float16 ones 2.3e-4 against 2.1e-4; float32 keeps three parts.
 #include <algorithm>
 #include <cmath>
 #include <new>
